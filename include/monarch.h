@@ -349,6 +349,39 @@ int monarch_to_dense(const void* R, const void* L, void* M,
 int monarch_project(const void* A, void* R, void* L, int n, int m,
                     monarch_dtype dtype, void* stream, unsigned flags);
 
+/* The loss behind the last layer of a language model: softmax cross entropy of a row's logits over a vocabulary,
+ *   l[t][v] = sum_i x[t][i] * W[v][i],   lse[t] = log sum_v exp l[t][v],   loss[t] = lse[t] - l[t][target[t]].
+ * x (rows, width), W (vocab, width) of `dtype`; target: rows int64; loss and lse: rows fp32.  The logits are never kept.
+ * A row whose target is `ignore_index` has no loss (0; its lse is written all the same); a target that is neither that nor
+ * an entry of the vocabulary gives NaN.  Products are accumulated in fp32; fp32 operands lose less than 2^-21 of each product.
+ * All pointers are device pointers, 16-byte aligned (loss, lse and target: 8).  `workspace` (256-byte aligned) holds
+ * monarch_xent_fwd_workspace_bytes(...) bytes; contents ignored on entry.  flags must be 0.  rows == 0 is a successful no-op.
+ * rows, vocab <= 2^20 and width <= 65536, else MONARCH_ERR_UNSUPPORTED. */
+int monarch_xent_fwd(const void* x, const void* W, const int64_t* target, float* loss, float* lse,
+                     int64_t rows, int vocab, int width, int64_t ignore_index,
+                     monarch_dtype dtype, void* stream, void* workspace, size_t workspace_bytes, unsigned flags);
+size_t monarch_xent_fwd_workspace_bytes(int64_t rows, int vocab, int width, monarch_dtype dtype, unsigned flags);
+
+/* Its gradients, from the lse of the forward:  G[t][v] = (exp(l[t][v] - lse[t]) - [v = target[t]]) * g[t],
+ *   dx = G W,   dW = G^T x,
+ * g[t] = dloss[t * dloss_stride] / *divisor (fp32 on the device; stride 0: one value for all rows; divisor NULL: 1), 0 for
+ * ignored rows, whose x has no influence on dW whatever it holds.  dx (rows, width) and dW (vocab, width) of `dtype` (dW fp32
+ * with MONARCH_FLAG_WGRAD_F32) are overwritten; either may be NULL.  The logits are computed a second time, a piece of the
+ * vocabulary after the other; in the bf16 path G is rounded to bf16.  `workspace`: the call runs best with
+ * monarch_xent_bwd_workspace_bytes(...) bytes and takes less, down to room for G of 256 entries of the vocabulary (in more pieces; in the
+ * bf16 path dx is then added up in fp32 there), below which it returns MONARCH_ERR_WORKSPACE. */
+int monarch_xent_bwd(const void* x, const void* W, const int64_t* target, const float* lse,
+                     const float* dloss, int64_t dloss_stride, const float* divisor, void* dx, void* dW,
+                     int64_t rows, int vocab, int width, int64_t ignore_index,
+                     monarch_dtype dtype, void* stream, void* workspace, size_t workspace_bytes, unsigned flags);
+size_t monarch_xent_bwd_workspace_bytes(int64_t rows, int vocab, int width, monarch_dtype dtype, unsigned flags);
+
+/* total[0] = the sum of the losses of the rows that are not ignored, or with mean != 0 their mean; total[1] = their number, at
+ * least 1 (the divisor of monarch_xent_bwd for a mean: a batch without a target has loss 0 and gradients 0).  total: two
+ * fp32, 8-byte aligned. */
+int monarch_xent_total(const float* loss, const int64_t* target, float* total, int64_t rows, int64_t ignore_index, int mean,
+                       void* stream);
+
 /* Complex-valued Monarch multiply.  The paper's results hold over the complex numbers as well
  * (Notation Review), and its MRI reconstruction model is a single complex Monarch matrix.  Same steps,
  * shapes and layouts as monarch_fwd_ex / monarch_bwd, every element a complex64 (two fp32: real part,

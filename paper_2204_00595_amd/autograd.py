@@ -44,6 +44,21 @@ def monarch_linear(x: torch.Tensor, R: torch.Tensor, L: torch.Tensor, bias: torc
     return binding._native_calls.linear(x, R, L, bias, save_intermediate)
 
 
+_REDUCTIONS = {"none": 0, "mean": 1, "sum": 2}
+
+
+def vocab_cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, ignore_index: int = -100,
+                        reduction: str = "mean") -> torch.Tensor:
+    """Cross entropy of the logits x weight^T against `target`, without the logits; differentiable in x and weight.
+
+    x (..., width) and weight (vocab, width) in fp32 or bf16, target (...) int64.  The loss is fp32: one for each row ("none"), or
+    the sum or mean over the rows whose target is not `ignore_index` (0 if there is none).  A target outside the vocabulary makes
+    the loss and the gradients NaN."""
+    if reduction not in _REDUCTIONS:
+        raise ValueError("reduction must be one of %s, got %r" % (", ".join(sorted(_REDUCTIONS)), reduction))
+    return binding._native_calls.vocab_loss(x, weight, target, ignore_index, _REDUCTIONS[reduction])
+
+
 class MonarchLinear(torch.nn.Module):
     """A linear layer whose weight is a Monarch matrix with `nblocks` blocks per factor.
 

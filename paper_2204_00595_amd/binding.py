@@ -36,6 +36,7 @@ EXPORTS = (
     "monarch_bwd_bias", "monarch_fwd_bias_gelu", "monarch_bwd_bias_gelu_in",
     "monarch_bwd_workspace_bytes",
     "monarch_fwd_t", "monarch_fwd_t_workspace_bytes", "monarch_saved_bytes", "monarch_fwd_save", "monarch_fwd_bias_save", "monarch_bwd_saved", "monarch_kept_bytes", "monarch_fwd_keep", "monarch_bwd_kept", "monarch_bwd_kept_workspace_bytes", "monarch_fwd_c64", "monarch_fwd_h_c64", "monarch_bwd_c64", "monarch_fwd_c64_ws", "monarch_fwd_h_c64_ws", "monarch_bwd_c64_ws", "monarch_c64_workspace_bytes", "monarch_dft_factors", "monarch_to_dense", "monarch_project", "monarch_kernel_name", "monarch_status_string", "monarch_version", "monarch_stream_copy", "monarch_launch_probe",
+    "monarch_xent_fwd", "monarch_xent_fwd_workspace_bytes", "monarch_xent_bwd", "monarch_xent_bwd_workspace_bytes", "monarch_xent_total",
 )
 
 _lib = None
@@ -123,6 +124,16 @@ def lib() -> ctypes.CDLL:
         L.monarch_dft_factors.argtypes = [vp, vp, ci, ci, vp]
         L.monarch_project.restype = ci
         L.monarch_project.argtypes = [vp, vp, vp, ci, ci, ci, vp, cu]
+        L.monarch_xent_fwd.restype = ci
+        L.monarch_xent_fwd.argtypes = [vp] * 5 + [i64, ci, ci, i64, ci, vp, vp, sz, cu]
+        L.monarch_xent_fwd_workspace_bytes.restype = sz
+        L.monarch_xent_fwd_workspace_bytes.argtypes = [i64, ci, ci, ci, cu]
+        L.monarch_xent_bwd.restype = ci
+        L.monarch_xent_bwd.argtypes = [vp] * 5 + [i64] + [vp] * 3 + [i64, ci, ci, i64, ci, vp, vp, sz, cu]
+        L.monarch_xent_bwd_workspace_bytes.restype = sz
+        L.monarch_xent_bwd_workspace_bytes.argtypes = [i64, ci, ci, ci, cu]
+        L.monarch_xent_total.restype = ci
+        L.monarch_xent_total.argtypes = [vp, vp, vp, i64, i64, ci, vp]
         L.monarch_kernel_name.restype = ctypes.c_char_p
         L.monarch_kernel_name.argtypes = [ci, ci, ci, ci, ci, ci, cu]
         L.monarch_status_string.restype = ctypes.c_char_p
@@ -374,3 +385,32 @@ def monarch_dft_factors(m: int, inverse: bool = False, device="cuda", stream=Non
     if rc != MONARCH_OK:
         raise MonarchError(rc, "monarch_dft_factors")
     return R, L
+
+
+def monarch_xent_fwd_workspace_bytes(rows: int, vocab: int, width: int, dtype: int, flags: int = 0) -> int:
+    return int(lib().monarch_xent_fwd_workspace_bytes(rows, vocab, width, dtype, flags))
+
+
+def monarch_xent_bwd_workspace_bytes(rows: int, vocab: int, width: int, dtype: int, flags: int = 0) -> int:
+    return int(lib().monarch_xent_bwd_workspace_bytes(rows, vocab, width, dtype, flags))
+
+
+def monarch_xent_fwd(x: torch.Tensor, W: torch.Tensor, target: torch.Tensor, loss: torch.Tensor | None = None,
+                     lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None, ignore_index: int = -100, stream=None):
+    """(loss, lse), fp32 (rows,): the cross entropy of the logits x W^T against `target` (int64), and the log of the sum of their
+    exponentials.  x (rows, width), W (vocab, width).  Rows whose target is `ignore_index` have loss 0."""
+    return _native_calls.xent_fwd(x, W, target, loss, lse, workspace, ignore_index, stream)
+
+
+def monarch_xent_bwd(x: torch.Tensor, W: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                     divisor: torch.Tensor | None = None, dx: torch.Tensor | None = None, dW: torch.Tensor | None = None,
+                     want_dx: bool = True, want_dW: bool = True, workspace: torch.Tensor | None = None, ignore_index: int = -100,
+                     flags: int = 0, stream=None):
+    """(dx, dW) for the upstream gradient dloss / divisor: dloss fp32 (rows,) or one value for all rows, divisor one fp32 value.
+    A gradient that is not wanted (and has no buffer) is None."""
+    return _native_calls.xent_bwd(x, W, target, lse, dloss, divisor, dx, dW, want_dx, want_dW, workspace, ignore_index, flags, stream)
+
+
+def monarch_xent_total(loss: torch.Tensor, target: torch.Tensor, ignore_index: int = -100, mean: bool = True, stream=None) -> torch.Tensor:
+    """fp32 (2,): the mean (or sum) of the losses of the rows that are not ignored, and their number (at least 1)."""
+    return _native_calls.xent_total(loss, target, ignore_index, mean, stream)

@@ -2,6 +2,7 @@
 // Everything here runs on the host; validation never touches the GPU.
 #include "../../include/monarch.h"
 #include "monarch_internal.h"
+#include "monarch_xent.h"
 
 #include <mutex>
 #include <vector>
@@ -687,6 +688,70 @@ int monarch_project(const void* A, void* R, void* L, int n, int m, monarch_dtype
     if (!aligned(A, 16) || !aligned(R, 16) || !aligned(L, 16)) return MONARCH_ERR_INVALID;
     if (!project_supported(m)) return MONARCH_ERR_UNSUPPORTED;
     return launch_project(A, R, L, m, (int)dtype, (hipStream_t)stream);
+}
+
+// ---- loss over a vocabulary ----
+
+namespace {
+
+int check_xent(int64_t rows, int vocab, int width, int dtype, unsigned flags, unsigned known)
+{
+    if (rows < 0 || vocab <= 0 || width <= 0) return MONARCH_ERR_INVALID;
+    if (dtype != MONARCH_F32 && dtype != MONARCH_BF16) return MONARCH_ERR_INVALID;
+    if (flags & ~known) return MONARCH_ERR_INVALID;
+    return xent_supported(rows, vocab, width) ? MONARCH_OK : MONARCH_ERR_UNSUPPORTED;
+}
+bool xent_pointers(const void* x, const void* W, const int64_t* target, const float* lse)
+{
+    return x && W && target && lse && aligned(x, 16) && aligned(W, 16) && aligned(target, 8) && aligned(lse, 8);
+}
+
+}  // namespace
+
+size_t monarch_xent_fwd_workspace_bytes(int64_t rows, int vocab, int width, monarch_dtype dtype, unsigned flags)
+{
+    return check_xent(rows, vocab, width, (int)dtype, flags, 0u) ? 0 : xent_fwd_workspace(rows, vocab, width, (int)dtype);
+}
+
+int monarch_xent_fwd(const void* x, const void* W, const int64_t* target, float* loss, float* lse, int64_t rows, int vocab, int width,
+                     int64_t ignore_index, monarch_dtype dtype, void* stream, void* workspace, size_t workspace_bytes, unsigned flags)
+{
+    if (int rc = check_xent(rows, vocab, width, (int)dtype, flags, 0u)) return rc;
+    if (rows == 0) return W ? MONARCH_OK : MONARCH_ERR_INVALID;
+    if (!xent_pointers(x, W, target, lse) || !loss || !aligned(loss, 8)) return MONARCH_ERR_INVALID;
+    if (!room_for(workspace, workspace_bytes, xent_fwd_workspace(rows, vocab, width, (int)dtype))) return MONARCH_ERR_WORKSPACE;
+    return xent_fwd(x, W, target, loss, lse, rows, vocab, width, ignore_index, (int)dtype, workspace, (hipStream_t)stream);
+}
+
+size_t monarch_xent_bwd_workspace_bytes(int64_t rows, int vocab, int width, monarch_dtype dtype, unsigned flags)
+{
+    return check_xent(rows, vocab, width, (int)dtype, flags, MONARCH_FLAG_WGRAD_F32) ? 0 : xent_bwd_workspace(rows, vocab, width, (int)dtype);
+}
+
+int monarch_xent_bwd(const void* x, const void* W, const int64_t* target, const float* lse, const float* dloss, int64_t dloss_stride,
+                     const float* divisor, void* dx, void* dW, int64_t rows, int vocab, int width, int64_t ignore_index, monarch_dtype dtype,
+                     void* stream, void* workspace, size_t workspace_bytes, unsigned flags)
+{
+    if (int rc = check_xent(rows, vocab, width, (int)dtype, flags, MONARCH_FLAG_WGRAD_F32)) return rc;
+    if ((dloss_stride != 0 && dloss_stride != 1) || !W || !aligned(dW, 16) || !aligned(dx, 16)) return MONARCH_ERR_INVALID;
+    const hipStream_t st = (hipStream_t)stream;
+    const bool f32 = dtype == MONARCH_F32 || (flags & MONARCH_FLAG_WGRAD_F32);
+    const size_t weights = (size_t)vocab * width;
+    if (rows == 0) {
+        if (!dW) return MONARCH_OK;
+        return f32 ? launch_fill_zero_f32((float*)dW, weights, st) : launch_fill_zero_u16((uint16_t*)dW, weights, st);
+    }
+    if (!xent_pointers(x, W, target, lse) || !dloss || !aligned(dloss, 4) || !aligned(divisor, 4)) return MONARCH_ERR_INVALID;
+    if (!dx && !dW) return MONARCH_OK;
+    if (!room_for(workspace, workspace_bytes, xent_bwd_least(rows, vocab, width, (int)dtype))) return MONARCH_ERR_WORKSPACE;
+    return xent_bwd(x, W, target, lse, dloss, dloss_stride, divisor, dx, dW, rows, vocab, width, ignore_index, (int)dtype, f32, workspace, workspace_bytes, st);
+}
+
+int monarch_xent_total(const float* loss, const int64_t* target, float* total, int64_t rows, int64_t ignore_index, int mean, void* stream)
+{
+    if (rows < 0 || !total || !aligned(total, 8)) return MONARCH_ERR_INVALID;
+    if (rows > 0 && (!loss || !target || !aligned(loss, 4) || !aligned(target, 8))) return MONARCH_ERR_INVALID;
+    return xent_total(loss, target, total, rows, ignore_index, mean != 0, (hipStream_t)stream);
 }
 
 const char* monarch_kernel_name(int pass, int n_in, int k, int q, int s, monarch_dtype dtype, unsigned flags)

@@ -483,6 +483,136 @@ struct LinearFn : torch::autograd::Function<LinearFn> {
     }
 };
 
+// ---- loss over a vocabulary ----
+
+struct VocabShape {  // x (rows, width), W (vocab, width), target (rows,)
+    int64_t rows, width, vocab;
+    at::ScalarType dtype;
+    c10::Device device;
+    VocabShape(const Tensor& x, const Tensor& W, const Tensor& target) : dtype(x.scalar_type()), device(x.device())
+    {
+        TORCH_CHECK_VALUE(x.dim() == 2 && W.dim() == 2, "x and W must have two dimensions");
+        rows = x.size(0);
+        width = x.size(1);
+        vocab = W.size(0);
+        TORCH_CHECK_TYPE(dtype == at::kFloat || dtype == at::kBFloat16, "dtype must be float32 or bfloat16, got ", dtype);
+        check(x, "x", {rows, width}, dtype, device);
+        check(W, "W", {vocab, width}, dtype, device);
+        check(target, "target", {rows}, at::kLong, device);
+        // (what the C ABI's int holds; it refuses what it cannot do)
+        TORCH_CHECK_VALUE(vocab <= INT32_MAX && width <= INT32_MAX, "x or W is too large");
+    }
+    monarch_dtype code() const { return dtype == at::kFloat ? MONARCH_F32 : MONARCH_BF16; }
+};
+
+struct RowLoss {
+    Tensor loss, lse;
+};
+RowLoss xent_fwd(const Tensor& x, const Tensor& W, const Tensor& target, RowLoss r, Tensor ws, int64_t ignore, const StreamArg& st)
+{
+    const Where w(x.device(), st);
+    const VocabShape sh(x, W, target);
+    r.loss = out(r.loss, "loss", {sh.rows}, at::kFloat, sh.device);
+    r.lse = out(r.lse, "lse", {sh.rows}, at::kFloat, sh.device);
+    if (!ws.defined()) {
+        const size_t need = monarch_xent_fwd_workspace_bytes(sh.rows, (int)sh.vocab, (int)sh.width, sh.code(), 0);
+        if (need) ws = w.scratch(need);
+    }
+    const Bytes b(ws);
+    const int rc = monarch_xent_fwd(ptr(x), ptr(W), target.data_ptr<int64_t>(), (float*)ptr(r.loss), (float*)ptr(r.lse), sh.rows, (int)sh.vocab,
+                                    (int)sh.width, ignore, sh.code(), w.stream(), b.p, b.n, 0);
+    if (rc) raise_status(rc, "monarch_xent_fwd");
+    return r;
+}
+
+struct VocabGrads {
+    Tensor dx, dW;
+};
+// dloss: (rows,), or one value for all of them; divisor: one value (may be missing)
+VocabGrads xent_bwd(const Tensor& x, const Tensor& W, const Tensor& target, const Tensor& lse, const Tensor& dloss, const Tensor& divisor,
+                    VocabGrads g, bool want_dx, bool want_dW, Tensor ws, int64_t ignore, unsigned flags, const StreamArg& st)
+{
+    const Where w(x.device(), st);
+    const VocabShape sh(x, W, target);
+    check(lse, "lse", {sh.rows}, at::kFloat, sh.device);
+    const bool one = dloss.numel() == 1 && (dloss.dim() == 0 || sh.rows != 1);
+    TORCH_CHECK_VALUE(dloss.device() == sh.device, "dloss must live on ", sh.device);
+    TORCH_CHECK_TYPE(dloss.scalar_type() == at::kFloat, "dloss: dtype ", dloss.scalar_type(), ", expected Float");
+    if (!one) check(dloss, "dloss", {sh.rows}, at::kFloat, sh.device);
+    if (divisor.defined()) {
+        TORCH_CHECK_VALUE(divisor.numel() == 1, "divisor must be one value");
+        check(divisor, "divisor", divisor.sizes(), at::kFloat, sh.device);
+    }
+    if (want_dx || g.dx.defined()) g.dx = out(g.dx, "dx", {sh.rows, sh.width}, sh.dtype, sh.device);
+    if (want_dW || g.dW.defined()) g.dW = out(g.dW, "dW", {sh.vocab, sh.width}, flags & MONARCH_FLAG_WGRAD_F32 ? at::kFloat : sh.dtype, sh.device);
+    if (!ws.defined()) {
+        const size_t need = monarch_xent_bwd_workspace_bytes(sh.rows, (int)sh.vocab, (int)sh.width, sh.code(), flags);
+        if (need) ws = w.scratch(need);
+    }
+    const Bytes b(ws);
+    const int rc = monarch_xent_bwd(ptr(x), ptr(W), target.data_ptr<int64_t>(), lse.data_ptr<float>(), (const float*)ptr(dloss), one ? 0 : 1,
+                                    (const float*)ptr(divisor), ptr(g.dx), ptr(g.dW), sh.rows, (int)sh.vocab, (int)sh.width, ignore,
+                                    sh.code(), w.stream(), b.p, b.n, flags);
+    if (rc) raise_status(rc, "monarch_xent_bwd");
+    return g;
+}
+
+// (sum or mean, number of rows that count)
+Tensor xent_total(const Tensor& loss, const Tensor& target, int64_t ignore, bool mean, const StreamArg& st)
+{
+    const Where w(loss.device(), st);
+    TORCH_CHECK_VALUE(loss.dim() == 1, "loss must have one dimension");
+    check(loss, "loss", loss.sizes(), at::kFloat, loss.device());
+    check(target, "target", loss.sizes(), at::kLong, loss.device());
+    const Tensor total = make({2}, at::kFloat, loss.device());
+    const int rc = monarch_xent_total((const float*)ptr(loss), target.data_ptr<int64_t>(), (float*)ptr(total), loss.size(0), ignore, mean, w.stream());
+    if (rc) raise_status(rc, "monarch_xent_total");
+    return total;
+}
+
+// contiguous and on 16 bytes, as the C ABI takes it
+Tensor dense(const Tensor& t)
+{
+    const Tensor c = t.contiguous();
+    return c.numel() && (uintptr_t)c.data_ptr() % 16 ? c.clone() : c;
+}
+
+enum Reduction { kNone, kMean, kSum };
+struct VocabLossFn : torch::autograd::Function<VocabLossFn> {
+    static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& x, const Tensor& W, const Tensor& target, int64_t ignore,
+                          int64_t reduction)
+    {
+        TORCH_CHECK_VALUE(x.dim() >= 1 && W.dim() == 2, "x must have a last dimension, W two");
+        const at::IntArrayRef leading = x.sizes().slice(0, x.dim() - 1);
+        TORCH_CHECK_VALUE(x.size(-1) == W.size(1), "the last dimension of x must be ", W.size(1), ", got shape ", x.sizes());
+        TORCH_CHECK_VALUE(target.sizes() == leading, "target: shape ", target.sizes(), ", expected ", leading);
+        int64_t rows = 1;
+        for (const int64_t n : leading) rows *= n;
+        const Tensor x2 = dense(x.reshape({rows, x.size(-1)})), W2 = dense(W), t2 = dense(target.reshape({rows}));
+        const StreamArg current;
+        const RowLoss r = xent_fwd(x2, W2, t2, {}, {}, ignore, current);
+        const Tensor total = reduction == kNone ? Tensor() : xent_total(r.loss, t2, ignore, reduction == kMean, current);
+        ctx->save_for_backward({x2, W2, t2, r.lse, reduction == kMean ? total.slice(0, 1, 2) : Tensor()});
+        ctx->saved_data["ignore"] = ignore;
+        ctx->saved_data["shape"] = x.sizes().vec();
+        return reduction == kNone ? r.loss.view(leading) : total.slice(0, 0, 1).view(at::IntArrayRef{});
+    }
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list dloss)
+    {
+        const auto saved = ctx->get_saved_variables();
+        const StreamArg current;
+        Tensor d = dloss[0].to(at::kFloat);
+        bool spread = d.dim() > 0 && d.numel() > 1;  // one value in every place (the gradient of a sum)
+        for (const int64_t s : d.strides()) spread = spread && s == 0;
+        if (spread) d = d.as_strided({}, {});
+        else if (d.dim() > 0) d = d.reshape({-1}).contiguous();
+        VocabGrads g = xent_bwd(saved[0], saved[1], saved[2], saved[3], d, saved[4], {}, ctx->needs_input_grad(0), ctx->needs_input_grad(1), {},
+                                ctx->saved_data["ignore"].toInt(), 0, current);
+        if (g.dx.defined()) g.dx = g.dx.view(ctx->saved_data["shape"].toIntVector());
+        return {g.dx, g.dW, Tensor(), Tensor(), Tensor()};
+    }
+};
+
 // ---- the Python module ----
 
 PyObject* none_or(const Tensor& t)
@@ -644,6 +774,53 @@ MONARCH_CALL(py_linear, 5)
     return THPVariable_Wrap(unlocked([&] { return LinearFn::apply(x, R, L, bias, save); }));
 MONARCH_END
 
+int64_t int_arg(PyObject* o)
+{
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw python_error();
+    return v;
+}
+
+// xent_fwd(x, W, target, loss, lse, workspace, ignore_index, stream)
+MONARCH_CALL(py_xent_fwd, 8)
+    const Tensor x = tensor_arg(a[0], "x"), W = tensor_arg(a[1], "W"), target = tensor_arg(a[2], "target"), ws = optional_arg(a[5], "workspace");
+    const RowLoss to{optional_arg(a[3], "loss"), optional_arg(a[4], "lse")};
+    const int64_t ignore = int_arg(a[6]);
+    const StreamArg st = stream_arg(a[7]);
+    const RowLoss r = unlocked([&] { return xent_fwd(x, W, target, to, ws, ignore, st); });
+    return tuple_of({r.loss, r.lse});
+MONARCH_END
+
+// xent_bwd(x, W, target, lse, dloss, divisor, dx, dW, want_dx, want_dW, workspace, ignore_index, flags, stream)
+MONARCH_CALL(py_xent_bwd, 14)
+    const Tensor x = tensor_arg(a[0], "x"), W = tensor_arg(a[1], "W"), target = tensor_arg(a[2], "target"), lse = tensor_arg(a[3], "lse"),
+                 dloss = tensor_arg(a[4], "dloss"), divisor = optional_arg(a[5], "divisor"), ws = optional_arg(a[10], "workspace");
+    const VocabGrads to{optional_arg(a[6], "dx"), optional_arg(a[7], "dW")};
+    const bool want_dx = bool_arg(a[8]), want_dW = bool_arg(a[9]);
+    const int64_t ignore = int_arg(a[11]);
+    const unsigned flags = flags_arg(a[12]);
+    const StreamArg st = stream_arg(a[13]);
+    const VocabGrads r =
+        unlocked([&] { return xent_bwd(x, W, target, lse, dloss, divisor, to, want_dx, want_dW, ws, ignore, flags, st); });
+    return tuple_of({r.dx, r.dW});
+MONARCH_END
+
+// xent_total(loss, target, ignore_index, mean, stream)
+MONARCH_CALL(py_xent_total, 5)
+    const Tensor loss = tensor_arg(a[0], "loss"), target = tensor_arg(a[1], "target");
+    const int64_t ignore = int_arg(a[2]);
+    const bool mean = bool_arg(a[3]);
+    const StreamArg st = stream_arg(a[4]);
+    return THPVariable_Wrap(unlocked([&] { return xent_total(loss, target, ignore, mean, st); }));
+MONARCH_END
+
+// vocab_loss(x, W, target, ignore_index, reduction)
+MONARCH_CALL(py_vocab_loss, 5)
+    const Tensor x = tensor_arg(a[0], "x"), W = tensor_arg(a[1], "W"), target = tensor_arg(a[2], "target");
+    const int64_t ignore = int_arg(a[3]), reduction = int_arg(a[4]);
+    return THPVariable_Wrap(unlocked([&] { return VocabLossFn::apply(x, W, target, ignore, reduction); }));
+MONARCH_END
+
 PyObject* py_set_error(PyObject*, PyObject* cls)
 {
     Py_INCREF(cls);
@@ -655,7 +832,8 @@ PyObject* py_set_error(PyObject*, PyObject* cls)
 PyMethodDef g_methods[] = {
     MONARCH_ENTRY(fwd), MONARCH_ENTRY(fwd_static), MONARCH_ENTRY(fwd_ws), MONARCH_ENTRY(fwd_bias), MONARCH_ENTRY(fwd_bias_gelu),
     MONARCH_ENTRY(fwd_t), MONARCH_ENTRY(fwd_save), MONARCH_ENTRY(bwd), MONARCH_ENTRY(to_dense), MONARCH_ENTRY(c64_apply),
-    MONARCH_ENTRY(c64_bwd), MONARCH_ENTRY(project), MONARCH_ENTRY(linear), {"set_error", py_set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    MONARCH_ENTRY(c64_bwd), MONARCH_ENTRY(project), MONARCH_ENTRY(linear),
+    MONARCH_ENTRY(xent_fwd), MONARCH_ENTRY(xent_bwd), MONARCH_ENTRY(xent_total), MONARCH_ENTRY(vocab_loss), {"set_error", py_set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,759 @@
+// Softmax cross entropy over a vocabulary, behind the last layer: logits l = x W^T (T x V), loss = log sum exp l - l[target], and its
+// gradients G = (exp(l - lse) - [v = target]) g, dx = G W, dW = G^T x.  The logits never exist in memory: the forward keeps the largest
+// and the sum of the exponentials of each 256 (or fewer) entries of the vocabulary a row, the backward computes the logits a second time
+// and holds G for a piece of the vocabulary.
+//
+// Every product is along the rows of its operands (monarch_nt.h), so what a product contracts over lies last: dx takes W^T, dW takes x^T
+// and G^T, laid out here.  fp32 operands are two binary16 planes: 22 bits of each number at three matrix products instead of the six
+// that three bf16 planes need; powers of two, one for each row that is not contracted over, keep them in binary16's range.
+#include "monarch_xent.h"
+#include "monarch_device.h"
+#include "monarch_nt.h"
+
+namespace monarch {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float log2_fast(float v) { return __builtin_amdgcn_logf(v); }
+
+__device__ __forceinline__ uint16_t f32_to_f16_bits(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+// the upper plane's number and what it leaves
+__device__ __forceinline__ void split2(float v, uint16_t& hi, uint16_t& lo)
+{
+    const _Float16 h = (_Float16)v;
+    hi = __builtin_bit_cast(uint16_t, h);
+    lo = f32_to_f16_bits(v - (float)h);
+}
+
+// Power of two that brings `top` (the largest finite magnitude) to 2^14 .. 2^15, and its inverse.
+__device__ __forceinline__ float scale_for(float top)
+{
+    const int e = (int)(__float_as_uint(top) >> 23) - 127;  // -127: zero and denormal numbers
+    int up = 14 - e;
+    up = top == 0.f ? 0 : up > 126 ? 126 : up;
+    return __uint_as_float((uint32_t)(up + 127) << 23);
+}
+__device__ __forceinline__ float inverse_power(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
+__device__ __forceinline__ float finite_magnitude(float v)
+{
+    const float a = fabsf(v);
+    return a < __builtin_inff() ? a : 0.f;  // (NaN compares false)
+}
+
+template <typename F>
+__device__ __forceinline__ float wave_all(float v, F f)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v = f(v, __shfl_xor(v, d));
+    return v;
+}
+__device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+
+// ---- operands ----
+
+// Rows of x or W as an operand: one wave a row.  bf16: copied, zeros up to whole steps.  fp32: two planes, the row's inverse power of two
+// in inv[row], its largest magnitude in top[row].
+template <typename T>
+__global__ __launch_bounds__(256) void pack_rows_kernel(const T* __restrict__ src, int64_t rows, int width, uint16_t* __restrict__ dst,
+                                                        uint32_t row_half, float* __restrict__ inv, float* __restrict__ top)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    const T* s = src + row * width;
+    uint16_t* d = dst + row * (int64_t)row_half;
+    if constexpr (sizeof(T) == 2) {
+        for (uint32_t k = lane; k < row_half; k += 64) d[k] = k < (uint32_t)width ? s[k] : (uint16_t)0;
+    } else {
+        float m = 0.f;
+        for (int k = lane; k < width; k += 64) m = fmaxf(m, finite_magnitude(s[k]));
+        m = wave_all(m, max_of);
+        const float up = scale_for(m);
+        if (lane == 0) {
+            inv[row] = inverse_power(up);
+            top[row] = m;
+        }
+        for (uint32_t k = lane; k < row_half / 2; k += 64) {
+            uint16_t hi = 0, lo = 0;
+            if (k < (uint32_t)width) split2(s[k] * up, hi, lo);
+            uint16_t* at = d + (k >> 5) * 64 + (k & 31);
+            at[0] = hi;
+            at[32] = lo;
+        }
+    }
+}
+
+// Columns of src (rows x width) as rows of an operand, 64 x 64 at a time.  `dl` (may be null): rows with dl = 0 count as zeros, whatever they
+// hold.  fp32: scaled by the power of two for *top.
+template <typename T>
+__global__ __launch_bounds__(256) void pack_columns_kernel(const T* __restrict__ src, int64_t rows, int width, uint16_t* __restrict__ dst,
+                                                           uint32_t row_half, const float* __restrict__ dl, const float* __restrict__ top)
+{
+    constexpr bool kPlanes = sizeof(T) == 4;
+    __shared__ T tile[64][sizeof(T) == 2 ? 66 : 65];
+    const int tid = threadIdx.x;
+    const int64_t k0 = (int64_t)blockIdx.x * 64;
+    const int c0 = blockIdx.y * 64;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int r = i * 4 + (tid >> 6), c = tid & 63;
+        T v = 0;
+        if (k0 + r < rows && c0 + c < width && !(dl && dl[k0 + r] == 0.f)) v = src[(k0 + r) * width + c0 + c];
+        tile[r][c] = v;
+    }
+    __syncthreads();
+    float up = 1.f;
+    if constexpr (kPlanes) up = scale_for(*top);
+    // eight along k of one column a piece
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int piece = i * 256 + tid, c = piece >> 3, r = (piece & 7) * 8;
+        if (c0 + c >= width) continue;
+        const int64_t k = k0 + r;
+        uint16_t hi[8], lo[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (kPlanes) split2(tile[r + e][c] * up, hi[e], lo[e]);
+            else hi[e] = tile[r + e][c];
+        }
+        uint16_t* d = dst + (int64_t)(c0 + c) * row_half;
+        if constexpr (kPlanes) {
+            uint16_t* at = d + (k >> 5) * 64 + (k & 31);
+            if (k * 2 < (int64_t)row_half) {
+                *reinterpret_cast<u32x4*>(at) = *reinterpret_cast<const u32x4*>(hi);
+                *reinterpret_cast<u32x4*>(at + 32) = *reinterpret_cast<const u32x4*>(lo);
+            }
+        } else if (k < (int64_t)row_half) {
+            *reinterpret_cast<u32x4*>(d + k) = *reinterpret_cast<const u32x4*>(hi);
+        }
+    }
+}
+
+// largest of n values (one workgroup)
+__global__ __launch_bounds__(1024) void largest_kernel(const float* __restrict__ v, int64_t n, const float* __restrict__ dl, float* __restrict__ out)
+{
+    __shared__ float part[16];
+    float m = 0.f;
+    for (int64_t i = threadIdx.x; i < n; i += 1024)
+        if (!dl || dl[i] != 0.f) m = fmaxf(m, v[i]);
+    m = wave_all(m, max_of);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; ++i) m = fmaxf(m, part[i]);
+        *out = m;
+    }
+}
+
+// ---- logits ----
+
+struct Logits {
+    NtOperand w, x;
+    const float *winv, *xinv;  // two planes: inverse powers of two of their rows
+    const int64_t* target;
+    int64_t rows;
+    int vocab, steps;
+    int v0, tiles_v, tiles_t;  // the piece of the vocabulary: entries v0 .. of it
+};
+
+template <typename C>
+__device__ __forceinline__ void logits_tile(const Logits& p, int64_t v0, int64_t t0, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ])
+{
+    nt_product<C>(p.w, v0, p.x, t0, 0, p.steps, lds, acc);
+    if constexpr (C::PL == 2) {
+        const int lane = threadIdx.x & 63;
+        float xi[C::TJ];
+#pragma unroll
+        for (int j = 0; j < C::TJ; ++j) {
+            const int64_t t = t0 + C::col0() + 16 * j + (lane & 15);
+            xi[j] = t < p.rows ? p.xinv[t] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t v = v0 + C::row0() + 16 * i + 4 * (lane >> 4) + e;
+                const float wi = v < p.vocab ? p.winv[v] : 0.f;
+#pragma unroll
+                for (int j = 0; j < C::TJ; ++j) acc[i][j][e] = acc[i][j][e] * wi * xi[j];
+            }
+    }
+}
+
+// Largest (in units of log 2) and sum of the tile's entries for each of its rows of x -> part[t][tile]; the target's logit -> hit[t].
+template <typename C>
+__global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* __restrict__ part, int parts, float* __restrict__ hit)
+{
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    int tv, tt;
+    if (!nt_place(blockIdx.x, p.tiles_v, p.tiles_t, tv, tt)) return;
+    const int64_t v0 = (int64_t)tv * C::BM, t0 = (int64_t)tt * C::BN;
+    f32x4 acc[C::TI][C::TJ];
+    logits_tile<C>(p, v0, t0, lds, acc);
+    const int lane = threadIdx.x & 63;
+    const int vr = C::row0() + 4 * (lane >> 4);
+    const int64_t left = p.vocab - v0 - vr;  // entries from the lane's first on
+    f32x2* red = reinterpret_cast<f32x2*>(lds);  // [BM / WM][BN]
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < C::TJ; ++j) {
+        const int64_t t = t0 + C::col0() + 16 * j + (lane & 15);
+        const int64_t at = t < p.rows ? p.target[t] - v0 - vr : -1;  // the target among the lane's entries
+        float m = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (at == 16 * i + e) hit[t] = acc[i][j][e];
+                if (16 * i + e >= left) acc[i][j][e] = -__builtin_inff();
+                m = fmaxf(m, acc[i][j][e]);
+            }
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        m *= kLog2e;
+        const float base = m == -__builtin_inff() ? 0.f : m;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s += exp2_fast(fmaf(acc[i][j][e], kLog2e, -base));
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        if (lane < 16) red[C::wave() / (C::BN / C::WN) * C::BN + C::col0() + 16 * j + lane] = f32x2{m, s};
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < C::BN; c += C::THREADS) {
+        const int64_t t = t0 + c;
+        if (t >= p.rows) break;
+        f32x2 r = red[c];
+#pragma unroll
+        for (int k = 1; k < C::BM / C::WM; ++k) {
+            const f32x2 o = red[k * C::BN + c];
+            const float m = fmaxf(r[0], o[0]), b = m == -__builtin_inff() ? 0.f : m;
+            r = f32x2{m, r[1] * exp2_fast(r[0] - b) + o[1] * exp2_fast(o[0] - b)};
+        }
+        part[t * parts + tv] = r;
+    }
+}
+
+// The parts of a row together: one wave a row.
+__global__ __launch_bounds__(256) void xent_join_kernel(const f32x2* __restrict__ part, int parts, const float* __restrict__ hit,
+                                                        const int64_t* __restrict__ target, int64_t ignore, int vocab, int64_t rows,
+                                                        float* __restrict__ loss, float* __restrict__ lse)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= rows) return;
+    const f32x2* p = part + t * parts;
+    float m = -__builtin_inff();
+    for (int i = lane; i < parts; i += 64) m = fmaxf(m, p[i][0]);
+    m = wave_all(m, max_of);
+    const float base = m == -__builtin_inff() ? 0.f : m;
+    float s = 0.f;
+    for (int i = lane; i < parts; i += 64) s += p[i][1] * exp2_fast(p[i][0] - base);
+    s = wave_all(s, sum_of);
+    if (lane) return;
+    const float all = (base + log2_fast(s)) * kLn2;
+    const int64_t at = target[t];
+    float l = 0.f;
+    if (at != ignore) l = at >= 0 && at < vocab ? all - hit[t] : __builtin_nanf("");
+    lse[t] = all;
+    loss[t] = l;
+}
+
+// ---- backward ----
+
+// Upstream gradient of each row -> dl: zero where ignored, NaN where the target is none.  out[0]: the largest magnitude.
+__global__ __launch_bounds__(1024) void xent_upstream_kernel(const float* __restrict__ dloss, int64_t stride, const float* __restrict__ divisor,
+                                                             const int64_t* __restrict__ target, int64_t ignore, int vocab, int64_t rows,
+                                                             float* __restrict__ dl, float* __restrict__ out)
+{
+    __shared__ float part[16];
+    const float by = divisor ? 1.f / *divisor : 1.f;
+    float m = 0.f;
+    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
+        const int64_t at = target[i];
+        float g = dloss[i * stride] * by;
+        if (at == ignore) g = 0.f;
+        else if (at < 0 || at >= vocab) g = __builtin_nanf("");
+        dl[i] = g;
+        m = fmaxf(m, finite_magnitude(g));
+    }
+    m = wave_all(m, max_of);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; ++i) m = fmaxf(m, part[i]);
+        *out = m;
+    }
+}
+
+// G of a piece of the vocabulary, once with the vocabulary last (g: rows of the piece's entries) and once with the rows of x last (gt), as
+// operands; both leave by way of LDS in runs of 64 bytes and more.  Entries and rows that do not exist are written as zeros.
+template <typename C>
+__global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const float* __restrict__ lse, const float* __restrict__ dl,
+                                                               const float* __restrict__ dl_top, uint16_t* __restrict__ g, uint32_t g_half,
+                                                               uint16_t* __restrict__ gt, uint32_t gt_half)
+{
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    int tv, tt;
+    if (!nt_place(blockIdx.x, p.tiles_v, p.tiles_t, tv, tt)) return;
+    const int64_t v0 = p.v0 + (int64_t)tv * C::BM, t0 = (int64_t)tt * C::BN;
+    f32x4 acc[C::TI][C::TJ];
+    logits_tile<C>(p, v0, t0, lds, acc);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int vr = C::row0() + 4 * (lane >> 4), tc = C::col0() + (lane & 15);
+    const int64_t left = p.vocab - v0 - vr;
+    float up = 1.f;
+    if constexpr (C::PL == 2) up = scale_for(*dl_top);
+#pragma unroll
+    for (int j = 0; j < C::TJ; ++j) {
+        const int64_t t = t0 + tc + 16 * j;
+        const bool row = t < p.rows;
+        const float ls = row ? lse[t] : 0.f, d = row ? dl[t] * up : 0.f;
+        const int64_t at = row ? p.target[t] - v0 - vr : -1;
+#pragma unroll
+        for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float s = exp2_fast((acc[i][j][e] - ls) * kLog2e);
+                if (at == 16 * i + e) s -= 1.f;
+                acc[i][j][e] = d == 0.f || 16 * i + e >= left ? 0.f : s * d;
+            }
+    }
+#pragma unroll
+    for (int plane = 0; plane < C::PL; ++plane) {
+        u32x2 v[C::TI][C::TJ];  // four entries of one row of x
+#pragma unroll
+        for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TJ; ++j) {
+                if constexpr (C::PL == 1) {
+                    v[i][j] = u32x2{pack_bf16x2(acc[i][j][0], acc[i][j][1]), pack_bf16x2(acc[i][j][2], acc[i][j][3])};
+                } else {
+                    uint32_t h[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const _Float16 f = (_Float16)acc[i][j][e];
+                        h[e] = __builtin_bit_cast(uint16_t, f);
+                        acc[i][j][e] -= (float)f;
+                    }
+                    v[i][j] = u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+                }
+            }
+        // 16-byte piece u of LDS row r in place u ^ (r % 16)
+        __syncthreads();
+        if (g) {
+#pragma unroll
+            for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+                for (int j = 0; j < C::TJ; ++j) {
+                    const int r = tc + 16 * j, e = vr + 16 * i;
+                    *reinterpret_cast<u32x2*>(lds + r * (2 * C::BM) + 16 * ((e >> 3) ^ (r & 15)) + 2 * (e & 4)) = v[i][j];
+                }
+            __syncthreads();
+            for (int at = tid; at < C::BN * (C::BM / 8); at += C::THREADS) {
+                const int r = at / (C::BM / 8), u = at % (C::BM / 8);
+                const int64_t k = (int64_t)tv * C::BM + 8 * u;
+                uint16_t* to = g + (t0 + r) * (int64_t)g_half + (C::PL == 1 ? k : (k >> 5) * 64 + 32 * plane + (k & 31));
+                *reinterpret_cast<u32x4*>(to) = lds128(lds + r * (2 * C::BM) + 16 * (u ^ (r & 15)));
+            }
+            __syncthreads();
+        }
+        if (!gt) continue;
+        // within four lanes (four rows of x) entries and rows change places
+#pragma unroll
+        for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TJ; ++j) {
+                const uint32_t a = v[i][j][0], b = v[i][j][1];
+                // with the neighbour: the even lane takes entries 0 and 2 of both rows, the odd lane 1 and 3
+                const uint32_t oa = __builtin_amdgcn_mov_dpp((int)a, 0xB1, 0xF, 0xF, true), ob = __builtin_amdgcn_mov_dpp((int)b, 0xB1, 0xF, 0xF, true);
+                const bool odd = lane & 1;
+                const uint32_t c = odd ? pick_hi16(oa, a) : pick_lo16(a, oa);  // entry 0 (1) of rows 2m, 2m + 1
+                const uint32_t d = odd ? pick_hi16(ob, b) : pick_lo16(b, ob);  // entry 2 (3)
+                // with the lane two on: the lower pair of lanes keeps entries 0 and 1, the upper pair 2 and 3
+                const uint32_t oc = __builtin_amdgcn_mov_dpp((int)c, 0x4E, 0xF, 0xF, true), od = __builtin_amdgcn_mov_dpp((int)d, 0x4E, 0xF, 0xF, true);
+                const bool upper = lane & 2;
+                const u32x2 four = upper ? u32x2{od, d} : u32x2{c, oc};
+                // lane q of the four holds entry (q % 2) + 2 (q / 2) = q of rows 0 .. 3
+                const int r = vr + 16 * i + (lane & 3), e = C::col0() + 16 * j + (lane & 12);
+                *reinterpret_cast<u32x2*>(lds + r * (2 * C::BN) + 16 * ((e >> 3) ^ (r & 7)) + 2 * (e & 4)) = four;
+            }
+        __syncthreads();
+        for (int at = tid; at < C::BM * (C::BN / 8); at += C::THREADS) {
+            const int r = at / (C::BN / 8), u = at % (C::BN / 8);
+            const int64_t k = t0 + 8 * u;
+            uint16_t* to = gt + ((int64_t)tv * C::BM + r) * gt_half + (C::PL == 1 ? k : (k >> 5) * 64 + 32 * plane + (k & 31));
+            *reinterpret_cast<u32x4*>(to) = lds128(lds + r * (2 * C::BN) + 16 * (u ^ (r & 7)));
+        }
+    }
+}
+
+// out[n][m] (rows of ld) = scale * sum over steps of A[m] B[n] (+ sum[n][m]), as OUT or, with `more`, as a running sum in fp32.
+template <typename C, typename OUT>
+__global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, NtOperand bn, int tiles_m, int tiles_n, int steps,
+                                                                  OUT* out, int64_t ld, float* sum, int add, int more,
+                                                                  const float* __restrict__ top_a, const float* __restrict__ top_b)
+{
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    int tm, tn;
+    if (!nt_place(blockIdx.x, tiles_m, tiles_n, tm, tn)) return;
+    f32x4 acc[C::TI][C::TJ];
+    nt_product<C>(am, (int64_t)tm * C::BM, bn, (int64_t)tn * C::BN, 0, steps, lds, acc);
+    float sa = 1.f, sb = 1.f;
+    if constexpr (C::PL == 2) {
+        sa = inverse_power(scale_for(*top_a));
+        sb = inverse_power(scale_for(*top_b));
+    }
+    const int lane = threadIdx.x & 63;
+    const int64_t m0 = (int64_t)tm * C::BM + C::row0() + 4 * (lane >> 4), n0 = (int64_t)tn * C::BN + C::col0() + (lane & 15);
+    const bool whole = (ld & 3) == 0;
+#pragma unroll
+    for (int j = 0; j < C::TJ; ++j) {
+        const int64_t n = n0 + 16 * j;
+        if (n >= bn.rows) continue;
+#pragma unroll
+        for (int i = 0; i < C::TI; ++i) {
+            const int64_t m = m0 + 16 * i;
+            if (m >= am.rows) continue;
+            f32x4 v = acc[i][j];
+            if constexpr (C::PL == 2) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = v[e] * sa * sb;
+            }
+            const int64_t at = n * ld + m;
+            if (whole) {
+                if (add) v += *reinterpret_cast<const f32x4*>(sum + at);
+                if (more) *reinterpret_cast<f32x4*>(sum + at) = v;
+                else if constexpr (sizeof(OUT) == 4) *reinterpret_cast<f32x4*>(out + at) = v;
+                else *reinterpret_cast<u32x2*>(out + at) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (m + e >= am.rows) break;
+                    if (add) v[e] += sum[at + e];
+                    if (more) sum[at + e] = v[e];
+                    else Elem<OUT>::store(out + at + e, v[e]);
+                }
+            }
+        }
+    }
+}
+
+// sum (or mean) of the losses of the rows that count, and their number (at least 1)
+__global__ __launch_bounds__(1024) void xent_total_kernel(const float* __restrict__ loss, const int64_t* __restrict__ target, int64_t ignore,
+                                                          int64_t rows, int mean, float* __restrict__ total)
+{
+    __shared__ double part[2][16];
+    double s = 0, c = 0;
+    for (int64_t i = threadIdx.x; i < rows; i += 1024)
+        if (target[i] != ignore) {
+            s += loss[i];
+            c += 1;
+        }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        s += __shfl_xor(s, d);
+        c += __shfl_xor(c, d);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        part[0][threadIdx.x >> 6] = s;
+        part[1][threadIdx.x >> 6] = c;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; ++i) {
+            s += part[0][i];
+            c += part[1][i];
+        }
+        c = c < 1 ? 1 : c;
+        total[0] = (float)(mean ? s / c : s);
+        total[1] = (float)c;
+    }
+}
+
+// ---- plans ----
+
+using Big = NtTile<256, 256, 128, 64, 1, false>;
+using Mid = NtTile<128, 128, 64, 64, 1, false>;
+using Low = NtTile<128, 64, 32, 64, 1, false>;
+using Big2 = NtTile<256, 256, 128, 64, 2, true>;
+using Mid2 = NtTile<128, 128, 64, 64, 2, true>;
+using Low2 = NtTile<128, 64, 32, 64, 2, true>;
+
+// bytes handed out of a workspace
+struct Area {
+    char* base;
+    size_t used = 0;
+    template <typename T>
+    T* take(size_t count)
+    {
+        T* p = base ? reinterpret_cast<T*>(base + used) : nullptr;
+        used += align_up(count * sizeof(T), 256);
+        return p;
+    }
+};
+
+struct Plan {
+    bool f32;
+    int64_t rows;
+    int vocab, width;
+    int per_step() const { return f32 ? 32 : 64; }  // numbers along k in a step
+    uint32_t half(int64_t k) const { return (uint32_t)((k + per_step() - 1) / per_step() * 64); }  // 16-bit numbers of an operand's row
+    // bf16 rows that are whole steps serve as they are
+    bool packs() const { return f32 || width % 64 != 0; }
+    // tile of the logits: 0 = 256 x 256, 1 = 128 x 128, 2 = 128 entries x 64 rows
+    int tile() const { return rows > 128 ? 0 : rows > 64 ? 1 : 2; }
+    int bv() const { return tile() == 0 ? 256 : 128; }
+    int bt() const { return tile() == 0 ? 256 : tile() == 1 ? 128 : 64; }
+    int parts() const { return (vocab + bv() - 1) / bv(); }
+    int64_t row_tiles() const { return (rows + bt() - 1) / bt(); }
+};
+
+struct Sides {  // x and W as operands, with their powers of two
+    uint16_t *x = nullptr, *w = nullptr;
+    float *xinv = nullptr, *winv = nullptr, *xtop = nullptr, *wtop = nullptr;
+    void lay(const Plan& p, Area& a)
+    {
+        if (!p.packs()) return;
+        x = a.take<uint16_t>((size_t)p.rows * p.half(p.width));
+        w = a.take<uint16_t>((size_t)p.vocab * p.half(p.width));
+        if (!p.f32) return;
+        xinv = a.take<float>(p.rows);
+        xtop = a.take<float>(p.rows);
+        winv = a.take<float>(p.vocab);
+        wtop = a.take<float>(p.vocab);
+    }
+};
+
+struct FwdArea {
+    Sides sides;
+    f32x2* part;
+    float* hit;
+    size_t lay(const Plan& p, char* base)
+    {
+        Area a{base};
+        sides.lay(p, a);
+        part = a.take<f32x2>((size_t)p.rows * p.parts());
+        hit = a.take<float>(p.rows);
+        return a.used;
+    }
+};
+
+constexpr size_t kPieceBytes = (size_t)1 << 30;  // G of a piece of the vocabulary, both ways round, where the workspace has room for it
+
+struct BwdArea {
+    Sides sides;
+    uint16_t *wt, *xt, *g, *gt;
+    float *dl, *tops, *sum;  // tops: dl, x, W
+    int piece;               // entries of the vocabulary, whole tiles
+    uint32_t g_half, gt_half, wt_half, xt_half;
+    size_t lay(const Plan& p, char* base, int64_t tiles_of_piece)
+    {
+        Area a{base};
+        sides.lay(p, a);
+        const int64_t tokens = p.row_tiles() * p.bt();
+        piece = (int)tiles_of_piece * p.bv();
+        g_half = p.half(piece);
+        gt_half = p.half(tokens);
+        wt_half = p.half((int64_t)p.parts() * p.bv());
+        xt_half = p.half(tokens);
+        wt = a.take<uint16_t>((size_t)p.width * wt_half);
+        xt = a.take<uint16_t>((size_t)p.width * xt_half);
+        g = a.take<uint16_t>((size_t)tokens * g_half);
+        gt = a.take<uint16_t>((size_t)piece * gt_half);
+        dl = a.take<float>(p.rows);
+        tops = a.take<float>(3);
+        sum = tiles_of_piece < p.parts() && !p.f32 ? a.take<float>((size_t)p.rows * p.width) : nullptr;
+        return a.used;
+    }
+    // Pieces of one length each, as few as kPieceBytes and a workspace of `room` bytes allow; 0: not even one tile of the vocabulary fits.
+    size_t fit(const Plan& p, char* base, size_t room)
+    {
+        const int64_t tiles = p.parts(), tokens = p.row_tiles() * p.bt();
+        int64_t most = (int64_t)(kPieceBytes / ((size_t)tokens * (p.f32 ? 8 : 4))) / p.bv();
+        most = most < 1 ? 1 : most > tiles ? tiles : most;
+        for (int64_t pieces = (tiles + most - 1) / most, last = 0; pieces <= tiles; ++pieces) {
+            const int64_t each = (tiles + pieces - 1) / pieces;
+            if (each == last) continue;
+            last = each;
+            const size_t need = lay(p, base, each);
+            if (need <= room) return need;
+        }
+        return 0;
+    }
+};
+
+int launched() { return hip_status(hipGetLastError()); }
+
+int pack_sides(const Plan& p, const Sides& s, const void* x, const void* w, hipStream_t st)
+{
+    if (!p.packs()) return 0;
+    const uint32_t half = p.half(p.width);
+    const dim3 gx((unsigned)((p.rows + 3) / 4)), gw((unsigned)((p.vocab + 3) / 4));
+    if (p.f32) {
+        pack_rows_kernel<float><<<gx, 256, 0, st>>>((const float*)x, p.rows, p.width, s.x, half, s.xinv, s.xtop);
+        pack_rows_kernel<float><<<gw, 256, 0, st>>>((const float*)w, p.vocab, p.width, s.w, half, s.winv, s.wtop);
+    } else {
+        pack_rows_kernel<uint16_t><<<gx, 256, 0, st>>>((const uint16_t*)x, p.rows, p.width, s.x, half, nullptr, nullptr);
+        pack_rows_kernel<uint16_t><<<gw, 256, 0, st>>>((const uint16_t*)w, p.vocab, p.width, s.w, half, nullptr, nullptr);
+    }
+    return launched();
+}
+
+Logits logits_of(const Plan& p, const Sides& s, const void* x, const void* w, const int64_t* target)
+{
+    const uint32_t bytes = p.half(p.width) * 2;
+    Logits l;
+    l.w = NtOperand{p.packs() ? s.w : w, p.vocab, bytes};
+    l.x = NtOperand{p.packs() ? s.x : x, p.rows, bytes};
+    l.winv = s.winv;
+    l.xinv = s.xinv;
+    l.target = target;
+    l.rows = p.rows;
+    l.vocab = p.vocab;
+    l.steps = (int)(bytes / 128);
+    l.v0 = 0;
+    l.tiles_v = p.parts();
+    l.tiles_t = (int)p.row_tiles();
+    return l;
+}
+
+template <typename C>
+int run_part(const Logits& l, f32x2* part, int parts, float* hit, hipStream_t st)
+{
+    if (allow_dynamic_lds((const void*)xent_part_kernel<C>, C::LDS_BYTES) != hipSuccess) return -4;
+    xent_part_kernel<C><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, part, parts, hit);
+    return launched();
+}
+template <typename C>
+int run_grad(const Logits& l, const float* lse, const BwdArea& a, uint16_t* g, uint16_t* gt, hipStream_t st)
+{
+    if (allow_dynamic_lds((const void*)xent_grad_kernel<C>, C::LDS_BYTES) != hipSuccess) return -4;
+    xent_grad_kernel<C><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, lse, a.dl, a.tops, g, a.g_half, gt, a.gt_half);
+    return launched();
+}
+template <typename C, typename OUT>
+int run_product(const NtOperand& a, const NtOperand& b, int steps, OUT* out, int64_t ld, float* sum, bool add, bool more, const float* top_a,
+                const float* top_b, hipStream_t st)
+{
+    if (allow_dynamic_lds((const void*)xent_product_kernel<C, OUT>, C::LDS_BYTES) != hipSuccess) return -4;
+    const int tm = (int)((a.rows + C::BM - 1) / C::BM), tn = (int)((b.rows + C::BN - 1) / C::BN);
+    xent_product_kernel<C, OUT><<<nt_grid(tm, tn), C::THREADS, C::LDS_BYTES, st>>>(a, b, tm, tn, steps, out, ld, sum, add, more, top_a, top_b);
+    return launched();
+}
+// The tile of a product by the number of workgroups: one of 256 x 256 a CU or two of 128 x 128.
+template <typename B, typename M, typename OUT>
+int product(const NtOperand& a, const NtOperand& b, int steps, OUT* out, int64_t ld, float* sum, bool add, bool more, const float* top_a,
+            const float* top_b, hipStream_t st)
+{
+    const int64_t big = ((a.rows + 255) / 256) * ((b.rows + 255) / 256), mid = ((a.rows + 127) / 128) * ((b.rows + 127) / 128);
+    if ((big + 255) / 256 * 4 <= (mid + 511) / 512 * 2) return run_product<B, OUT>(a, b, steps, out, ld, sum, add, more, top_a, top_b, st);
+    return run_product<M, OUT>(a, b, steps, out, ld, sum, add, more, top_a, top_b, st);
+}
+
+}  // namespace
+
+bool xent_supported(int64_t rows, int vocab, int width)
+{
+    return rows <= (1 << 20) && vocab <= (1 << 20) && width <= (1 << 16);
+}
+
+size_t xent_fwd_workspace(int64_t rows, int vocab, int width, int dtype)
+{
+    FwdArea a;
+    return rows ? a.lay(Plan{dtype == 0, rows, vocab, width}, nullptr) : 0;
+}
+size_t xent_bwd_workspace(int64_t rows, int vocab, int width, int dtype)
+{
+    BwdArea a;
+    return rows ? a.fit(Plan{dtype == 0, rows, vocab, width}, nullptr, (size_t)-1) : 0;
+}
+size_t xent_bwd_least(int64_t rows, int vocab, int width, int dtype)
+{
+    BwdArea a;
+    return rows ? a.lay(Plan{dtype == 0, rows, vocab, width}, nullptr, 1) : 0;
+}
+
+int xent_fwd(const void* x, const void* w, const int64_t* target, float* loss, float* lse, int64_t rows, int vocab, int width, int64_t ignore,
+             int dtype, void* ws, hipStream_t st)
+{
+    const Plan p{dtype == 0, rows, vocab, width};
+    FwdArea a;
+    a.lay(p, (char*)ws);
+    if (int rc = pack_sides(p, a.sides, x, w, st)) return rc;
+    const Logits l = logits_of(p, a.sides, x, w, target);
+    const int parts = p.parts(), tile = p.tile();
+    int rc;
+    if (p.f32) rc = tile == 0 ? run_part<Big2>(l, a.part, parts, a.hit, st) : tile == 1 ? run_part<Mid2>(l, a.part, parts, a.hit, st) : run_part<Low2>(l, a.part, parts, a.hit, st);
+    else rc = tile == 0 ? run_part<Big>(l, a.part, parts, a.hit, st) : tile == 1 ? run_part<Mid>(l, a.part, parts, a.hit, st) : run_part<Low>(l, a.part, parts, a.hit, st);
+    if (rc) return rc;
+    xent_join_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a.part, parts, a.hit, target, ignore, vocab, rows, loss, lse);
+    return launched();
+}
+
+int xent_bwd(const void* x, const void* w, const int64_t* target, const float* lse, const float* dloss, int64_t dloss_stride, const float* divisor,
+             void* dx, void* dw, int64_t rows, int vocab, int width, int64_t ignore, int dtype, bool dw_f32, void* ws, size_t ws_bytes, hipStream_t st)
+{
+    const Plan p{dtype == 0, rows, vocab, width};
+    BwdArea a;
+    if (!a.fit(p, (char*)ws, ws_bytes)) return -3;
+    xent_upstream_kernel<<<1, 1024, 0, st>>>(dloss, dloss_stride, divisor, target, ignore, vocab, rows, a.dl, a.tops);
+    if (int rc = launched()) return rc;
+    if (int rc = pack_sides(p, a.sides, x, w, st)) return rc;
+    if (p.f32) {
+        largest_kernel<<<1, 1024, 0, st>>>(a.sides.xtop, rows, a.dl, a.tops + 1);
+        largest_kernel<<<1, 1024, 0, st>>>(a.sides.wtop, vocab, nullptr, a.tops + 2);
+    }
+    const unsigned columns = (unsigned)((width + 63) / 64);
+    auto pack_columns = [&](const void* src, int64_t n, uint16_t* to, uint32_t half, const float* dl, const float* top) {
+        const dim3 grid((unsigned)((half / (p.f32 ? 2 : 1) + 63) / 64), columns);
+        if (p.f32) pack_columns_kernel<float><<<grid, 256, 0, st>>>((const float*)src, n, width, to, half, dl, top);
+        else pack_columns_kernel<uint16_t><<<grid, 256, 0, st>>>((const uint16_t*)src, n, width, to, half, dl, top);
+    };
+    if (dx) pack_columns(w, vocab, a.wt, a.wt_half, nullptr, a.tops + 2);
+    if (dw) pack_columns(x, rows, a.xt, a.xt_half, a.dl, a.tops + 1);
+    if (int rc = launched()) return rc;
+    Logits l = logits_of(p, a.sides, x, w, target);
+    const int tile = p.tile(), per = p.per_step();
+    for (int v0 = 0; v0 < vocab; v0 += a.piece) {
+        const int entries = vocab - v0 < a.piece ? vocab - v0 : a.piece;
+        l.v0 = v0;
+        l.tiles_v = (entries + p.bv() - 1) / p.bv();
+        uint16_t *g = dx ? a.g : nullptr, *gt = dw ? a.gt : nullptr;
+        int rc;
+        if (p.f32) rc = tile == 0 ? run_grad<Big2>(l, lse, a, g, gt, st) : tile == 1 ? run_grad<Mid2>(l, lse, a, g, gt, st) : run_grad<Low2>(l, lse, a, g, gt, st);
+        else rc = tile == 0 ? run_grad<Big>(l, lse, a, g, gt, st) : tile == 1 ? run_grad<Mid>(l, lse, a, g, gt, st) : run_grad<Low>(l, lse, a, g, gt, st);
+        if (rc) return rc;
+        if (dx) {
+            // features inside, rows of x outside
+            const NtOperand A{a.wt + (size_t)v0 / per * 64, width, a.wt_half * 2}, B{a.g, rows, a.g_half * 2};
+            const int steps = (entries + per - 1) / per;
+            const bool first = v0 == 0, last = v0 + a.piece >= vocab;
+            if (p.f32) rc = product<Big2, Mid2, float>(A, B, steps, (float*)dx, width, (float*)dx, !first, false, a.tops + 2, a.tops, st);
+            else rc = product<Big, Mid, uint16_t>(A, B, steps, (uint16_t*)dx, width, a.sum, !first, !last, nullptr, nullptr, st);
+            if (rc) return rc;
+        }
+        if (dw) {
+            const NtOperand A{a.xt, width, a.xt_half * 2}, B{a.gt, entries, a.gt_half * 2};
+            const int steps = (int)((rows + per - 1) / per);
+            const size_t at = (size_t)v0 * width;
+            if (p.f32) rc = product<Big2, Mid2, float>(A, B, steps, (float*)dw + at, width, nullptr, false, false, a.tops + 1, a.tops, st);
+            else if (dw_f32) rc = product<Big, Mid, float>(A, B, steps, (float*)dw + at, width, nullptr, false, false, nullptr, nullptr, st);
+            else rc = product<Big, Mid, uint16_t>(A, B, steps, (uint16_t*)dw + at, width, nullptr, false, false, nullptr, nullptr, st);
+            if (rc) return rc;
+        }
+    }
+    return 0;
+}
+
+int xent_total(const float* loss, const int64_t* target, float* total, int64_t rows, int64_t ignore, bool mean, hipStream_t st)
+{
+    xent_total_kernel<<<1, 1024, 0, st>>>(loss, target, ignore, rows, mean, total);
+    return launched();
+}
+
+}  // namespace monarch

@@ -382,6 +382,32 @@ size_t monarch_xent_bwd_workspace_bytes(int64_t rows, int vocab, int width, mona
 int monarch_xent_total(const float* loss, const int64_t* target, float* total, int64_t rows, int64_t ignore_index, int mean,
                        void* stream);
 
+/* An update made orthogonal by Newton-Schulz steps, block by block: G is a stack of `blocks` blocks of m x n (a Monarch factor;
+ * blocks = 1: a dense matrix), and each becomes
+ *   X_0 = G / (|G|_F + eps),   then `steps` times   X <- a X + (b A + c A^2) X,  A = X X^T (X^T X where m > n),
+ * with (a, b, c) = coefficients: the singular values move towards 1, the singular vectors stay, so that a block-diagonal matrix
+ * gets the nearest orthogonal one of its kind.  G and X (blocks, m, n) of `dtype`, X overwritten.  The Frobenius norm is summed in
+ * 64 bits, the operands of the products have 22 bits, sums are fp32.
+ * The coefficients have to keep singular values from [0, 1] below 2 (3.4445, -4.7750, 2.0315 and 1.875, -1.25, 0.375 do);
+ * |a| + 2 |b| + 4 |c| > 100, steps < 1 and eps < 0 are MONARCH_ERR_INVALID.  A block of zeros stays zero (eps > 0); a block that
+ * holds something not finite comes out not finite, the others are as without it.  m, n <= 16384 and blocks <= 65535, else
+ * MONARCH_ERR_UNSUPPORTED.  `coefficients` is host memory.  blocks == 0 is a successful no-op. */
+int monarch_orthogonalize(const void* G, void* X, int64_t blocks, int m, int n, const float* coefficients, int steps, float eps,
+                          monarch_dtype dtype, void* stream, void* workspace, size_t workspace_bytes);
+size_t monarch_orthogonalize_workspace_bytes(int64_t blocks, int m, int n, monarch_dtype dtype);
+
+/* One step of the optimiser that follows orthogonalised momenta, on `count` tensors of one shape (blocks, m, n) at once:
+ *   V <- momentum V + G,   U = G + momentum V (nesterov != 0) or V,   W <- (1 - lr decay) W - lr scale X(U)
+ * with X as above.  weights, grads, momenta, masters: host arrays of `count` device pointers (the tensors may lie anywhere; 16-byte
+ * aligned; no two outputs may overlap).  V is fp32.  W is of `dtype`, G of `grad_dtype`.  With `masters` (fp32 (blocks, m, n); W bf16) the
+ * step is made on the master and W becomes its rounding; NULL: on W itself, which in bf16 loses updates below its rounding.
+ * Every tensor is updated once, in place. */
+int monarch_muon_step(int count, void* const* weights, const void* const* grads, float* const* momenta, float* const* masters,
+                      int64_t blocks, int m, int n, float lr, float momentum, float decay, float scale, int nesterov,
+                      const float* coefficients, int steps, float eps, monarch_dtype dtype, monarch_dtype grad_dtype,
+                      void* stream, void* workspace, size_t workspace_bytes);
+size_t monarch_muon_step_workspace_bytes(int count, int64_t blocks, int m, int n, monarch_dtype dtype, int with_masters);
+
 /* Complex-valued Monarch multiply.  The paper's results hold over the complex numbers as well
  * (Notation Review), and its MRI reconstruction model is a single complex Monarch matrix.  Same steps,
  * shapes and layouts as monarch_fwd_ex / monarch_bwd, every element a complex64 (two fp32: real part,

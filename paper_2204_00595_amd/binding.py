@@ -10,6 +10,7 @@ library is missing, loading fails with an error that says how to build it.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -37,6 +38,7 @@ EXPORTS = (
     "monarch_bwd_workspace_bytes",
     "monarch_fwd_t", "monarch_fwd_t_workspace_bytes", "monarch_saved_bytes", "monarch_fwd_save", "monarch_fwd_bias_save", "monarch_bwd_saved", "monarch_kept_bytes", "monarch_fwd_keep", "monarch_bwd_kept", "monarch_bwd_kept_workspace_bytes", "monarch_fwd_c64", "monarch_fwd_h_c64", "monarch_bwd_c64", "monarch_fwd_c64_ws", "monarch_fwd_h_c64_ws", "monarch_bwd_c64_ws", "monarch_c64_workspace_bytes", "monarch_dft_factors", "monarch_to_dense", "monarch_project", "monarch_kernel_name", "monarch_status_string", "monarch_version", "monarch_stream_copy", "monarch_launch_probe",
     "monarch_xent_fwd", "monarch_xent_fwd_workspace_bytes", "monarch_xent_bwd", "monarch_xent_bwd_workspace_bytes", "monarch_xent_total",
+    "monarch_orthogonalize", "monarch_orthogonalize_workspace_bytes", "monarch_muon_step", "monarch_muon_step_workspace_bytes",
 )
 
 _lib = None
@@ -134,6 +136,15 @@ def lib() -> ctypes.CDLL:
         L.monarch_xent_bwd_workspace_bytes.argtypes = [i64, ci, ci, ci, cu]
         L.monarch_xent_total.restype = ci
         L.monarch_xent_total.argtypes = [vp, vp, vp, i64, i64, ci, vp]
+        cf = ctypes.c_float
+        L.monarch_orthogonalize.restype = ci
+        L.monarch_orthogonalize.argtypes = [vp, vp, i64, ci, ci, vp, ci, cf, ci, vp, vp, sz]
+        L.monarch_orthogonalize_workspace_bytes.restype = sz
+        L.monarch_orthogonalize_workspace_bytes.argtypes = [i64, ci, ci, ci]
+        L.monarch_muon_step.restype = ci
+        L.monarch_muon_step.argtypes = [ci] + [vp] * 4 + [i64, ci, ci] + [cf] * 4 + [ci, vp, ci, cf, ci, ci, vp, vp, sz]
+        L.monarch_muon_step_workspace_bytes.restype = sz
+        L.monarch_muon_step_workspace_bytes.argtypes = [ci, i64, ci, ci, ci, ci]
         L.monarch_kernel_name.restype = ctypes.c_char_p
         L.monarch_kernel_name.argtypes = [ci, ci, ci, ci, ci, ci, cu]
         L.monarch_status_string.restype = ctypes.c_char_p
@@ -414,3 +425,36 @@ def monarch_xent_bwd(x: torch.Tensor, W: torch.Tensor, target: torch.Tensor, lse
 def monarch_xent_total(loss: torch.Tensor, target: torch.Tensor, ignore_index: int = -100, mean: bool = True, stream=None) -> torch.Tensor:
     """fp32 (2,): the mean (or sum) of the losses of the rows that are not ignored, and their number (at least 1)."""
     return _native_calls.xent_total(loss, target, ignore_index, mean, stream)
+
+
+# a s + b s^3 + c s^5: steep at 0, so that five steps bring singular values from 0.01 on to between 0.7 and 1.2
+MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+def monarch_orthogonalize_workspace_bytes(blocks: int, m: int, n: int, dtype: int) -> int:
+    return int(lib().monarch_orthogonalize_workspace_bytes(blocks, m, n, dtype))
+
+
+def monarch_muon_step_workspace_bytes(count: int, blocks: int, m: int, n: int, dtype: int, with_masters: bool = False) -> int:
+    return int(lib().monarch_muon_step_workspace_bytes(count, blocks, m, n, dtype, 1 if with_masters else 0))
+
+
+def monarch_orthogonalize(G: torch.Tensor, X: torch.Tensor | None = None, steps: int = 5, coefficients=MUON_COEFFICIENTS,
+                          eps: float = 1e-7, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Each block of G (blocks, m, n), or G (m, n) itself, over its Frobenius norm and through `steps` Newton-Schulz steps: its singular
+    values near 1, its singular vectors kept."""
+    return _native_calls.orthogonalize(G, X, coefficients, steps, eps, workspace, stream)
+
+
+def monarch_muon_step(weights, grads, momenta, lr: float, momentum: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
+                      scale: float | None = None, steps: int = 5, coefficients=MUON_COEFFICIENTS, eps: float = 1e-7, masters=None,
+                      workspace: torch.Tensor | None = None, stream=None) -> None:
+    """One step on lists of tensors of one shape, (blocks, m, n) or (m, n), in place:
+
+    momentum v <- momentum v + grad; the weight (its fp32 master, where `masters` are given for bf16 weights) shrinks by lr weight_decay and
+    moves by lr scale against the orthogonalised grad + momentum v (without `nesterov`: v).  `scale`: sqrt(max(1, m / n)) unless given.
+    momenta are fp32, grads fp32 or bf16."""
+    if scale is None:
+        scale = math.sqrt(max(1.0, weights[0].shape[-2] / weights[0].shape[-1])) if len(weights) else 1.0
+    _native_calls.muon_step(weights, grads, momenta, masters, lr, momentum, weight_decay, scale, nesterov, coefficients, steps, eps,
+                            workspace, stream)

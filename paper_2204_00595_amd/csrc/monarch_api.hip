@@ -2,6 +2,7 @@
 // Everything here runs on the host; validation never touches the GPU.
 #include "../../include/monarch.h"
 #include "monarch_internal.h"
+#include "monarch_ortho.h"
 #include "monarch_xent.h"
 
 #include <mutex>
@@ -752,6 +753,85 @@ int monarch_xent_total(const float* loss, const int64_t* target, float* total, i
     if (rows < 0 || !total || !aligned(total, 8)) return MONARCH_ERR_INVALID;
     if (rows > 0 && (!loss || !target || !aligned(loss, 4) || !aligned(target, 8))) return MONARCH_ERR_INVALID;
     return xent_total(loss, target, total, rows, ignore_index, mean != 0, (hipStream_t)stream);
+}
+
+// ---- orthogonalised updates ----
+
+namespace {
+
+int check_ortho(OrthoShape& s, int count, int64_t blocks, int m, int n, int dtype, bool masters)
+{
+    if (count < 0 || blocks < 0 || m <= 0 || n <= 0) return MONARCH_ERR_INVALID;
+    if (dtype != MONARCH_F32 && dtype != MONARCH_BF16) return MONARCH_ERR_INVALID;
+    if (masters && dtype != MONARCH_BF16) return MONARCH_ERR_INVALID;
+    if (blocks > 65535) return MONARCH_ERR_UNSUPPORTED;
+    // as many tensors at a time as one launch takes
+    const int64_t fit = blocks ? 65535 / blocks : count;
+    s = OrthoShape{blocks, m, n, (int)(count < kOrthoTensors ? count : kOrthoTensors)};
+    if (s.count > fit) s.count = (int)fit;
+    return ortho_supported(s) ? MONARCH_OK : MONARCH_ERR_UNSUPPORTED;
+}
+int check_steps(OrthoSteps& k, const float* c, int steps, float eps)
+{
+    if (!c || steps < 1 || !(eps >= 0.f)) return MONARCH_ERR_INVALID;
+    const float size = (c[0] < 0 ? -c[0] : c[0]) + 2 * (c[1] < 0 ? -c[1] : c[1]) + 4 * (c[2] < 0 ? -c[2] : c[2]);
+    if (!(size <= 100.f)) return MONARCH_ERR_INVALID;
+    k = OrthoSteps{c[0], c[1], c[2], eps, steps};
+    return MONARCH_OK;
+}
+
+}  // namespace
+
+size_t monarch_orthogonalize_workspace_bytes(int64_t blocks, int m, int n, monarch_dtype dtype)
+{
+    OrthoShape s;
+    return check_ortho(s, 1, blocks, m, n, (int)dtype, false) ? 0 : ortho_workspace(s);
+}
+
+int monarch_orthogonalize(const void* G, void* X, int64_t blocks, int m, int n, const float* coefficients, int steps, float eps,
+                          monarch_dtype dtype, void* stream, void* workspace, size_t workspace_bytes)
+{
+    OrthoShape s;
+    OrthoSteps k;
+    if (int rc = check_ortho(s, 1, blocks, m, n, (int)dtype, false)) return rc;
+    if (int rc = check_steps(k, coefficients, steps, eps)) return rc;
+    if (blocks == 0) return MONARCH_OK;
+    if (!G || !X || !aligned(G, 16) || !aligned(X, 16)) return MONARCH_ERR_INVALID;
+    if (!room_for(workspace, workspace_bytes, ortho_workspace(s))) return MONARCH_ERR_WORKSPACE;
+    return ortho_run(s, k, G, X, dtype == MONARCH_BF16, workspace, (hipStream_t)stream);
+}
+
+size_t monarch_muon_step_workspace_bytes(int count, int64_t blocks, int m, int n, monarch_dtype dtype, int with_masters)
+{
+    OrthoShape s;
+    return check_ortho(s, count, blocks, m, n, (int)dtype, with_masters != 0) ? 0 : ortho_workspace(s);
+}
+
+int monarch_muon_step(int count, void* const* weights, const void* const* grads, float* const* momenta, float* const* masters, int64_t blocks,
+                      int m, int n, float lr, float momentum, float decay, float scale, int nesterov, const float* coefficients, int steps,
+                      float eps, monarch_dtype dtype, monarch_dtype grad_dtype, void* stream, void* workspace, size_t workspace_bytes)
+{
+    OrthoShape s;
+    OrthoSteps k;
+    if (int rc = check_ortho(s, count, blocks, m, n, (int)dtype, masters != nullptr)) return rc;
+    if (grad_dtype != MONARCH_F32 && grad_dtype != MONARCH_BF16) return MONARCH_ERR_INVALID;
+    if (int rc = check_steps(k, coefficients, steps, eps)) return rc;
+    if (count == 0 || blocks == 0) return MONARCH_OK;
+    if (!weights || !grads || !momenta) return MONARCH_ERR_INVALID;
+    for (int i = 0; i < count; ++i) {
+        if (!weights[i] || !grads[i] || !momenta[i] || (masters && !masters[i])) return MONARCH_ERR_INVALID;
+        if (!aligned(weights[i], 16) || !aligned(grads[i], 16) || !aligned(momenta[i], 16) || (masters && !aligned(masters[i], 16)))
+            return MONARCH_ERR_INVALID;
+    }
+    if (!room_for(workspace, workspace_bytes, ortho_workspace(s))) return MONARCH_ERR_WORKSPACE;
+    const MuonRule rule{lr, momentum, decay, scale, nesterov != 0};
+    for (int i = 0, each = s.count; i < count; i += each) {
+        s.count = count - i < each ? count - i : each;
+        const int rc = muon_run(s, k, rule, weights + i, grads + i, momenta + i, masters ? masters + i : nullptr, dtype == MONARCH_BF16,
+                                grad_dtype == MONARCH_BF16, workspace, (hipStream_t)stream);
+        if (rc) return rc;
+    }
+    return MONARCH_OK;
 }
 
 const char* monarch_kernel_name(int pass, int n_in, int k, int q, int s, monarch_dtype dtype, unsigned flags)

@@ -1,0 +1,32 @@
+// Orthogonalised updates (monarch_ortho.hip): what the C ABI calls after its checks.
+#pragma once
+#include "monarch_internal.h"
+
+namespace monarch {
+
+struct OrthoShape {
+    int64_t blocks;  // of one tensor
+    int m, n;        // a block
+    int count;       // tensors
+    int64_t all() const { return blocks * count; }
+};
+struct OrthoSteps {
+    float a, b, c, eps;
+    int steps;
+};
+struct MuonRule {
+    float lr, momentum, decay, scale;
+    bool nesterov;
+};
+
+constexpr int kOrthoTensors = 48;  // of one launch
+
+bool ortho_supported(const OrthoShape& s);
+size_t ortho_workspace(const OrthoShape& s);
+// g, x: one tensor, fp32 or (bf16) bf16
+int ortho_run(const OrthoShape& s, const OrthoSteps& k, const void* g, void* x, bool bf16, void* ws, hipStream_t st);
+// count <= kOrthoTensors; masters (null: none) are fp32, weights then bf16
+int muon_run(const OrthoShape& s, const OrthoSteps& k, const MuonRule& rule, void* const* weights, const void* const* grads, float* const* momenta,
+             float* const* masters, bool weights_bf16, bool grads_bf16, void* ws, hipStream_t st);
+
+}  // namespace monarch

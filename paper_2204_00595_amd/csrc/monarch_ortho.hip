@@ -1,0 +1,430 @@
+// Orthogonalised updates.  A block G (m x n) becomes X_0 = G / (|G|_F + eps), and each step takes X to
+//   X' = a X + (b A + c A^2) X,   A = X X^T,
+// which moves every singular value s to a s + b s^3 + c s^5 and leaves the singular vectors.  A is taken on the shorter side, r = min(m, n);
+// below X is r x c (the transpose of the block where it is higher than wide).
+//
+// Three products a step, all along the rows of their operands (monarch_nt.h): A = X X^T, P = a I + b A + c A A^T (A is symmetric), X' = P X
+// with X kept both ways round.  Operands are binary16 numbers times a power of two, in two planes: entries of X and A are below 2, those
+// of P below |a| + 2 |b| + 4 |c|, and 22 bits of each are kept (five steps of the 3.4445, -4.7750, 2.0315 polynomial lose 2.5e-7 of the
+// result's norm, fp32 products 1e-6 to 2e-6).  bf16 gradients take the same: with one plane (11 bits) the result would be 1.0e-3 to
+// 1.5e-3 off beside its own rounding of 1.7e-3, and far more where a few directions stand out, since small singular values grow up to
+// 485 times and the rounding of the large ones with them.
+#include "monarch_ortho.h"
+#include "monarch_device.h"
+#include "monarch_nt.h"
+
+#include <utility>
+
+namespace monarch {
+namespace {
+
+constexpr float kX = 0x1p11f, kA = 0x1p11f, kP = 0x1p9f;  // what X, A and P are stored times
+
+// 16-bit numbers of an operand's row of k numbers, and where number k of a plane lies in it
+__host__ __device__ __forceinline__ uint32_t row_half(int k) { return (uint32_t)((k + 31) / 32 * 64); }
+__device__ __forceinline__ uint32_t place(uint32_t k, int plane) { return (k >> 5) * 64 + 32 * plane + (k & 31); }
+
+__device__ __forceinline__ uint32_t f16_bits(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+__device__ __forceinline__ float f16_value(uint32_t h) { return (float)__builtin_bit_cast(_Float16, (uint16_t)h); }
+
+// four numbers -> their upper plane (packed); v becomes what that leaves
+__device__ __forceinline__ u32x2 take_plane(f32x4& v)
+{
+    uint32_t h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        h[e] = f16_bits(v[e]);
+        v[e] -= f16_value(h[e]);
+    }
+    return u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+}
+// Among four lanes (4q .. 4q + 3) with four 16-bit numbers each: lane i gets number i of all four.
+__device__ __forceinline__ u32x2 change_places(u32x2 v)
+{
+    const int lane = threadIdx.x;
+    const uint32_t a = v[0], b = v[1];
+    const uint32_t oa = __builtin_amdgcn_mov_dpp((int)a, 0xB1, 0xF, 0xF, true), ob = __builtin_amdgcn_mov_dpp((int)b, 0xB1, 0xF, 0xF, true);
+    const uint32_t c = lane & 1 ? pick_hi16(oa, a) : pick_lo16(a, oa), d = lane & 1 ? pick_hi16(ob, b) : pick_lo16(b, ob);
+    const uint32_t oc = __builtin_amdgcn_mov_dpp((int)c, 0x4E, 0xF, 0xF, true), od = __builtin_amdgcn_mov_dpp((int)d, 0x4E, 0xF, 0xF, true);
+    return lane & 2 ? u32x2{od, d} : u32x2{c, oc};
+}
+
+// ---- norm, momentum, first operands ----
+
+constexpr int kChunk = 4096;  // numbers of a block that a workgroup adds up
+
+struct Source {  // tensors of `blocks` blocks of m x n
+    const void* g[kOrthoTensors];
+    float* v[kOrthoTensors];  // momenta (MUON)
+    int blocks;
+    int m, n;
+    float momentum;
+    int nesterov;
+};
+
+__device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
+__device__ __forceinline__ f32x4 load4(const uint16_t* p)
+{
+    const u32x2 u = *reinterpret_cast<const u32x2*>(p);
+    return f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xffff0000u)};
+}
+
+// v <- momentum v + g, and the sum of the squares of the update's numbers (g + momentum v, or v; without momentum: g) of a chunk, in 64 bits:
+// no gradient that fp32 holds is too large or too small for its square.
+template <typename T, bool MUON>
+__global__ __launch_bounds__(256) void ortho_norm_kernel(Source s, double* __restrict__ part)
+{
+    __shared__ double wave[4];
+    const int block = blockIdx.y, tensor = block / s.blocks;
+    const int64_t size = (int64_t)s.m * s.n, at = (int64_t)(block - tensor * s.blocks) * size;
+    const T* g = (const T*)s.g[tensor] + at;
+    float* v = MUON ? s.v[tensor] + at : nullptr;
+    const int64_t from = (int64_t)blockIdx.x * kChunk, to = size - from < kChunk ? size : from + kChunk;
+    double sum = 0;
+    auto update = [&](float gi, float& vi) {
+        if constexpr (!MUON) return gi;
+        vi = fmaf(s.momentum, vi, gi);
+        return s.nesterov ? fmaf(s.momentum, vi, gi) : vi;
+    };
+    if ((size & 3) == 0) {
+        for (int64_t i = from + 4 * threadIdx.x; i < to; i += 1024) {
+            const f32x4 gi = load4(g + i);
+            f32x4 vi = {};
+            if constexpr (MUON) vi = load4(v + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float ve = vi[e];
+                const double u = update(gi[e], ve);
+                vi[e] = ve;
+                sum += u * u;
+            }
+            if constexpr (MUON) *reinterpret_cast<f32x4*>(v + i) = vi;
+        }
+    } else {
+        for (int64_t i = from + threadIdx.x; i < to; i += 256) {
+            float vi = MUON ? v[i] : 0.f;
+            const double u = update(Elem<T>::load(g + i), vi);
+            if constexpr (MUON) v[i] = vi;
+            sum += u * u;
+        }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) part[(int64_t)block * gridDim.x + blockIdx.x] = wave[0] + wave[1] + wave[2] + wave[3];
+}
+
+// The update over its norm as operands, rows as they are (along: m rows of n) and columns (across: n rows of m), 64 x 64 at a time; zeros up to
+// whole steps.
+template <typename T, bool MUON>
+__global__ __launch_bounds__(256) void ortho_pack_kernel(Source s, const double* __restrict__ part, int parts, float eps,
+                                                         uint16_t* __restrict__ along, uint16_t* __restrict__ across)
+{
+    __shared__ float tile[64][65];
+    __shared__ double wave[4];
+    const int block = blockIdx.z, tensor = block / s.blocks, tid = threadIdx.x;
+    const int64_t size = (int64_t)s.m * s.n, at = (int64_t)(block - tensor * s.blocks) * size;
+    const T* g = (const T*)s.g[tensor] + at;
+    const float* v = MUON ? s.v[tensor] + at : nullptr;
+    double sum = 0;
+    for (int i = tid; i < parts; i += 256) sum += part[(int64_t)block * parts + i];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if ((tid & 63) == 0) wave[tid >> 6] = sum;
+    __syncthreads();
+    const double by = (double)kX / (sqrt(wave[0] + wave[1] + wave[2] + wave[3]) + (double)eps);
+    const int i0 = blockIdx.x * 64, j0 = blockIdx.y * 64;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const int i = i0 + 4 * k + (tid >> 6), j = j0 + (tid & 63);
+        float u = 0.f;
+        if (i < s.m && j < s.n) {
+            const int64_t p = (int64_t)i * s.n + j;
+            const float gi = Elem<T>::load(g + p);
+            u = gi;
+            if constexpr (MUON) u = s.nesterov ? fmaf(s.momentum, v[p], gi) : v[p];
+            u = (float)(u * by);
+        }
+        tile[4 * k + (tid >> 6)][tid & 63] = u;
+    }
+    __syncthreads();
+    const uint32_t half_n = row_half(s.n), half_m = row_half(s.m);
+    along += (int64_t)block * s.m * half_n;
+    across += (int64_t)block * s.n * half_m;
+#pragma unroll
+    for (int way = 0; way < 2; ++way) {
+        const int row0 = way ? j0 : i0, col0 = way ? i0 : j0, rows = way ? s.n : s.m;
+        const uint32_t half = way ? half_m : half_n;
+        uint16_t* to = way ? across : along;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int piece = 256 * k + tid, r = piece >> 4, c = (piece & 15) * 4;
+            if (row0 + r >= rows || (uint32_t)(col0 + c) * 2 >= half) continue;
+            f32x4 u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = way ? tile[c + e][r] : tile[r][c + e];
+#pragma unroll
+            for (int plane = 0; plane < 2; ++plane)
+                *reinterpret_cast<u32x2*>(to + (int64_t)(row0 + r) * half + place(col0 + c, plane)) = take_plane(u);
+        }
+    }
+}
+
+// ---- products ----
+
+enum Part { kGram, kPoly, kNext, kLast };
+
+struct Product {
+    const uint16_t *a, *b;  // operands of all blocks: rows of them, 16-bit numbers a row
+    int a_rows, b_rows;
+    uint32_t half;          // of both
+    int tiles_a, tiles_b, blocks;
+    uint16_t *rows, *cols;  // results as operands: row b of them, and (kNext) row a of them
+    uint32_t rows_half, cols_half;
+    const uint16_t* gram;   // kPoly
+    float ca, cb, cc;
+};
+struct Sink {  // kLast: out[b][a], rows of n
+    void* out[kOrthoTensors];
+    float* master[kOrthoTensors];
+    int blocks;
+    int m, n;
+    float keep, rate;  // w <- keep w - rate x
+};
+enum Out { kPlain, kWeights, kMasters };  // x itself; weights updated; fp32 masters updated, weights their rounding
+
+template <typename C, Part PART, typename T, Out OUT>
+__global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Sink sink)
+{
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    // a block's tiles lie together on an XCD
+    const int tiles = p.tiles_a * p.tiles_b, total = tiles * p.blocks, each = (total + 7) >> 3;
+    const int t = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= each || t >= total) return;
+    const int block = t / tiles, in = t - block * tiles, tb = in / p.tiles_a, ta = in - tb * p.tiles_a;
+    const NtOperand a{p.a + (int64_t)block * p.a_rows * p.half, p.a_rows, p.half * 2}, b{p.b + (int64_t)block * p.b_rows * p.half, p.b_rows, p.half * 2};
+    f32x4 acc[C::TI][C::TJ];
+    nt_product<C>(a, (int64_t)ta * C::BM, b, (int64_t)tb * C::BN, 0, (int)(p.half / 64), lds, acc);
+    const int lane = threadIdx.x & 63;
+    const int m0 = ta * C::BM + C::row0() + 4 * (lane >> 4), n0 = tb * C::BN + C::col0() + (lane & 15);
+#pragma unroll
+    for (int j = 0; j < C::TJ; ++j)
+#pragma unroll
+        for (int i = 0; i < C::TI; ++i) {
+            const int m = m0 + 16 * i, n = n0 + 16 * j;
+            f32x4 v = acc[i][j];
+            if constexpr (PART == kLast) {
+                if (n >= p.b_rows) continue;
+                const int tensor = block / sink.blocks;
+                const int64_t at = (int64_t)(block - tensor * sink.blocks) * sink.m * sink.n + (int64_t)n * sink.n + m;
+                T* out = (T*)sink.out[tensor] + at;
+                float* master = OUT == kMasters ? sink.master[tensor] + at : nullptr;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (m + e >= p.a_rows) break;
+                    float x = v[e] * (1.f / (kX * kP));
+                    if constexpr (OUT == kWeights) x = fmaf(-sink.rate, x, sink.keep * Elem<T>::load(out + e));
+                    if constexpr (OUT == kMasters) master[e] = x = fmaf(-sink.rate, x, sink.keep * master[e]);
+                    Elem<T>::store(out + e, x);
+                }
+            } else {
+                // (what lies past a row's numbers is zero: the rows that do not exist were read as zeros)
+                const bool in_rows = n < p.b_rows && (uint32_t)m * 2 < p.rows_half;
+                uint16_t* row = p.rows + ((int64_t)block * p.b_rows + n) * p.rows_half;
+                if constexpr (PART == kGram) v *= kA / (kX * kX);
+                if constexpr (PART == kNext) v *= 1.f / kP;
+                if constexpr (PART == kPoly) {
+                    v *= p.cc * (kP / (kA * kA));
+                    if (in_rows) {
+                        const uint16_t* g = p.gram + ((int64_t)block * p.b_rows + n) * p.rows_half;
+#pragma unroll
+                        for (int plane = 0; plane < 2; ++plane) {
+                            const u32x2 u = *reinterpret_cast<const u32x2*>(g + place(m, plane));
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[e] = fmaf(p.cb * (kP / kA), f16_value(u[e >> 1] >> (16 * (e & 1))), v[e]);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (m + e == n) v[e] = fmaf(p.ca, kP, v[e]);
+                    }
+                }
+#pragma unroll
+                for (int plane = 0; plane < 2; ++plane) {
+                    const u32x2 u = take_plane(v);
+                    if (in_rows) *reinterpret_cast<u32x2*>(row + place(m, plane)) = u;
+                    if constexpr (PART == kNext) {
+                        const u32x2 w = change_places(u);
+                        const int r = m + (lane & 3), c = n & ~3;
+                        if (r < p.a_rows && (uint32_t)c * 2 < p.cols_half)
+                            *reinterpret_cast<u32x2*>(p.cols + ((int64_t)block * p.a_rows + r) * p.cols_half + place(c, plane)) = w;
+                    }
+                }
+            }
+        }
+}
+
+// ---- plan ----
+
+struct OrthoArea {
+    double* part;
+    int parts;
+    uint16_t *xr[2], *xt[2], *gram, *poly;
+    uint32_t half_r, half_c;
+    int r, c;
+    size_t lay(const OrthoShape& s, char* base)
+    {
+        size_t used = 0;
+        auto take = [&](size_t bytes) {
+            char* p = base ? base + used : nullptr;
+            used += align_up(bytes, 256);
+            return p;
+        };
+        r = s.m < s.n ? s.m : s.n;
+        c = s.m < s.n ? s.n : s.m;
+        half_r = row_half(r);
+        half_c = row_half(c);
+        parts = (int)(((int64_t)s.m * s.n + kChunk - 1) / kChunk);
+        part = (double*)take(s.all() * parts * sizeof(double));
+        for (int i = 0; i < 2; ++i) {
+            xr[i] = (uint16_t*)take((size_t)s.all() * r * half_c * 2);
+            xt[i] = (uint16_t*)take((size_t)s.all() * c * half_r * 2);
+        }
+        gram = (uint16_t*)take((size_t)s.all() * r * half_r * 2);
+        poly = (uint16_t*)take((size_t)s.all() * r * half_r * 2);
+        return used;
+    }
+};
+
+int launched() { return hip_status(hipGetLastError()); }
+
+template <typename C, Part PART, typename T, Out OUT>
+int run_product(Product p, const Sink& sink, hipStream_t st)
+{
+    if (allow_dynamic_lds((const void*)ortho_product_kernel<C, PART, T, OUT>, C::LDS_BYTES) != hipSuccess) return -4;
+    p.tiles_a = (p.a_rows + C::BM - 1) / C::BM;
+    p.tiles_b = (p.b_rows + C::BN - 1) / C::BN;
+    const unsigned grid = (unsigned)((p.tiles_a * p.tiles_b * p.blocks + 7) / 8 * 8);
+    ortho_product_kernel<C, PART, T, OUT><<<grid, C::THREADS, C::LDS_BYTES, st>>>(p, sink);
+    return launched();
+}
+template <Part PART, typename T, Out OUT>
+int product(const Product& p, const Sink& sink, hipStream_t st)
+{
+    using Low = NtTile<64, 64, 32, 32, 2, true>;
+    using Mid = NtTile<128, 128, 64, 64, 2, true>;
+    const int64_t mid = (int64_t)((p.a_rows + 127) / 128) * ((p.b_rows + 127) / 128) * p.blocks;
+    return mid >= 256 ? run_product<Mid, PART, T, OUT>(p, sink, st) : run_product<Low, PART, T, OUT>(p, sink, st);
+}
+
+template <typename T, Out OUT>
+int steps_of(const OrthoShape& s, const OrthoSteps& k, OrthoArea& a, const Sink& sink, hipStream_t st)
+{
+    const bool tall = s.m > s.n;
+    Product p{};
+    p.blocks = (int)s.all();
+    p.ca = k.a;
+    p.cb = k.b;
+    p.cc = k.c;
+    for (int i = 0; i < k.steps; ++i) {
+        const int at = i & 1;
+        Product gram = p, poly = p, next = p;
+        gram.a = gram.b = a.xr[at];
+        gram.a_rows = gram.b_rows = poly.a_rows = poly.b_rows = a.r;
+        gram.half = a.half_c;
+        gram.rows = a.gram;
+        gram.rows_half = poly.half = poly.rows_half = a.half_r;
+        poly.a = poly.b = poly.gram = a.gram;
+        poly.rows = a.poly;
+        if (int rc = product<kGram, uint16_t, kPlain>(gram, sink, st)) return rc;
+        if (int rc = product<kPoly, uint16_t, kPlain>(poly, sink, st)) return rc;
+        next.half = a.half_r;
+        next.a = a.poly;
+        next.a_rows = a.r;
+        next.b = a.xt[at];
+        next.b_rows = a.c;
+        if (i + 1 < k.steps) {
+            next.rows = a.xt[at ^ 1];
+            next.rows_half = a.half_r;
+            next.cols = a.xr[at ^ 1];
+            next.cols_half = a.half_c;
+            if (int rc = product<kNext, uint16_t, kPlain>(next, sink, st)) return rc;
+        } else {
+            // out[b][a]: the side that lies last in memory is a
+            if (!tall) {
+                std::swap(next.a, next.b);
+                std::swap(next.a_rows, next.b_rows);
+            }
+            if (int rc = product<kLast, T, OUT>(next, sink, st)) return rc;
+        }
+    }
+    return 0;
+}
+
+template <typename T, bool MUON>
+int first_operands(const OrthoShape& s, const OrthoSteps& k, const Source& src, const OrthoArea& a, hipStream_t st)
+{
+    const bool tall = s.m > s.n;
+    const unsigned all = (unsigned)s.all();
+    ortho_norm_kernel<T, MUON><<<dim3((unsigned)a.parts, all), 256, 0, st>>>(src, a.part);
+    ortho_pack_kernel<T, MUON><<<dim3((s.m + 63) / 64, (s.n + 63) / 64, all), 256, 0, st>>>(src, a.part, a.parts, k.eps, tall ? a.xt[0] : a.xr[0],
+                                                                                               tall ? a.xr[0] : a.xt[0]);
+    return launched();
+}
+
+}  // namespace
+
+bool ortho_supported(const OrthoShape& s)
+{
+    return s.m <= (1 << 14) && s.n <= (1 << 14) && s.all() <= 65535 && s.all() * s.m * s.n <= ((int64_t)1 << 33);
+}
+size_t ortho_workspace(const OrthoShape& s)
+{
+    OrthoArea a;
+    return s.all() ? a.lay(s, nullptr) : 0;
+}
+
+int ortho_run(const OrthoShape& s, const OrthoSteps& k, const void* g, void* x, bool bf16, void* ws, hipStream_t st)
+{
+    OrthoArea a;
+    a.lay(s, (char*)ws);
+    Source src{};
+    src.g[0] = g;
+    src.blocks = (int)s.blocks;
+    src.m = s.m;
+    src.n = s.n;
+    Sink sink{};
+    sink.out[0] = x;
+    sink.blocks = (int)s.blocks;
+    sink.m = s.m;
+    sink.n = s.n;
+    if (int rc = bf16 ? first_operands<uint16_t, false>(s, k, src, a, st) : first_operands<float, false>(s, k, src, a, st)) return rc;
+    return bf16 ? steps_of<uint16_t, kPlain>(s, k, a, sink, st) : steps_of<float, kPlain>(s, k, a, sink, st);
+}
+
+int muon_run(const OrthoShape& s, const OrthoSteps& k, const MuonRule& rule, void* const* weights, const void* const* grads, float* const* momenta,
+             float* const* masters, bool weights_bf16, bool grads_bf16, void* ws, hipStream_t st)
+{
+    OrthoArea a;
+    a.lay(s, (char*)ws);
+    Source src{};
+    Sink sink{};
+    for (int i = 0; i < s.count; ++i) {
+        src.g[i] = grads[i];
+        src.v[i] = momenta[i];
+        sink.out[i] = weights[i];
+        sink.master[i] = masters ? masters[i] : nullptr;
+    }
+    src.blocks = sink.blocks = (int)s.blocks;
+    src.m = sink.m = s.m;
+    src.n = sink.n = s.n;
+    src.momentum = rule.momentum;
+    src.nesterov = rule.nesterov;
+    sink.keep = 1.f - rule.lr * rule.decay;
+    sink.rate = rule.lr * rule.scale;
+    if (int rc = grads_bf16 ? first_operands<uint16_t, true>(s, k, src, a, st) : first_operands<float, true>(s, k, src, a, st)) return rc;
+    if (masters) return steps_of<uint16_t, kMasters>(s, k, a, sink, st);
+    return weights_bf16 ? steps_of<uint16_t, kWeights>(s, k, a, sink, st) : steps_of<float, kWeights>(s, k, a, sink, st);
+}
+
+}  // namespace monarch

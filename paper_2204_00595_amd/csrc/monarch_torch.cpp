@@ -18,6 +18,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <vector>
 
 #include "../../include/monarch.h"
 
@@ -613,6 +614,97 @@ struct VocabLossFn : torch::autograd::Function<VocabLossFn> {
     }
 };
 
+// ---- orthogonalised updates ----
+
+struct Blocks {  // (blocks, m, n), or (m, n): one block
+    int64_t blocks, m, n;
+    explicit Blocks(const Tensor& t, const char* name)
+    {
+        TORCH_CHECK_VALUE(t.dim() == 2 || t.dim() == 3, name, " must have two or three dimensions, got shape ", t.sizes());
+        blocks = t.dim() == 3 ? t.size(0) : 1;
+        m = t.size(-2);
+        n = t.size(-1);
+        TORCH_CHECK_VALUE(m > 0 && n > 0 && m <= INT32_MAX && n <= INT32_MAX, name, ": blocks of shape ", m, " x ", n);
+    }
+};
+monarch_dtype code_of(const Tensor& t, const char* name)
+{
+    TORCH_CHECK_TYPE(t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16, name, ": dtype must be float32 or bfloat16, got ",
+                     t.scalar_type());
+    return t.scalar_type() == at::kFloat ? MONARCH_F32 : MONARCH_BF16;
+}
+struct Steps {
+    float c[3], eps;
+    int steps;
+};
+
+Tensor orthogonalize(const Tensor& G, Tensor X, const Steps& k, Tensor ws, const StreamArg& st)
+{
+    const Where w(G.device(), st);
+    const Blocks b(G, "G");
+    const monarch_dtype code = code_of(G, "G");
+    check(G, "G", G.sizes(), G.scalar_type(), G.device());
+    X = out(X, "X", G.sizes(), G.scalar_type(), G.device());
+    if (!ws.defined()) {
+        const size_t need = monarch_orthogonalize_workspace_bytes(b.blocks, (int)b.m, (int)b.n, code);
+        if (need) ws = w.scratch(need);
+    }
+    const Bytes area(ws);
+    const int rc = monarch_orthogonalize(ptr(G), ptr(X), b.blocks, (int)b.m, (int)b.n, k.c, k.steps, k.eps, code, w.stream(), area.p, area.n);
+    if (rc) raise_status(rc, "monarch_orthogonalize");
+    return X;
+}
+
+struct MuonTensors {
+    std::vector<Tensor> weights, grads, momenta, masters;  // masters: none, or as many
+};
+struct MuonNumbers {
+    float lr, momentum, decay, scale;
+    bool nesterov;
+};
+void muon_step(const MuonTensors& t, const MuonNumbers& r, const Steps& k, Tensor ws, const StreamArg& st)
+{
+    const size_t count = t.weights.size();
+    TORCH_CHECK_VALUE(t.grads.size() == count && t.momenta.size() == count && (t.masters.empty() || t.masters.size() == count),
+                      "weights, grads, momenta and masters must be of one length");
+    if (!count) return;
+    const Tensor& first = t.weights[0];
+    const Where w(first.device(), st);
+    const Blocks b(first, "weights");
+    const monarch_dtype code = code_of(first, "weights"), grad_code = code_of(t.grads[0], "grads");
+    TORCH_CHECK_TYPE(t.masters.empty() || code == MONARCH_BF16, "masters go with bfloat16 weights");
+    std::vector<void*> wp(count);
+    std::vector<const void*> gp(count);
+    std::vector<float*> vp(count), mp(t.masters.size());
+    for (size_t i = 0; i < count; ++i) {
+        check(t.weights[i], "weights", first.sizes(), first.scalar_type(), first.device());
+        check(t.grads[i], "grads", first.sizes(), t.grads[0].scalar_type(), first.device());
+        check(t.momenta[i], "momenta", first.sizes(), at::kFloat, first.device());
+        wp[i] = t.weights[i].data_ptr();
+        gp[i] = t.grads[i].data_ptr();
+        vp[i] = t.momenta[i].data_ptr<float>();
+        if (t.masters.empty()) continue;
+        check(t.masters[i], "masters", first.sizes(), at::kFloat, first.device());
+        mp[i] = t.masters[i].data_ptr<float>();
+    }
+    if (!ws.defined()) {
+        const size_t need = monarch_muon_step_workspace_bytes((int)count, b.blocks, (int)b.m, (int)b.n, code, !t.masters.empty());
+        if (need) ws = w.scratch(need);
+    }
+    const Bytes area(ws);
+    const int rc = monarch_muon_step((int)count, wp.data(), gp.data(), vp.data(), t.masters.empty() ? nullptr : mp.data(), b.blocks, (int)b.m,
+                                     (int)b.n, r.lr, r.momentum, r.decay, r.scale, r.nesterov, k.c, k.steps, k.eps, code, grad_code, w.stream(),
+                                     area.p, area.n);
+    if (rc) raise_status(rc, "monarch_muon_step");
+    // (written behind autograd's back)
+    const auto written = [](const Tensor& x) {
+        if (!x.is_inference()) x.unsafeGetTensorImpl()->bump_version();
+    };
+    std::for_each(t.weights.begin(), t.weights.end(), written);
+    std::for_each(t.momenta.begin(), t.momenta.end(), written);
+    std::for_each(t.masters.begin(), t.masters.end(), written);
+}
+
 // ---- the Python module ----
 
 PyObject* none_or(const Tensor& t)
@@ -821,6 +913,57 @@ MONARCH_CALL(py_vocab_loss, 5)
     return THPVariable_Wrap(unlocked([&] { return VocabLossFn::apply(x, W, target, ignore, reduction); }));
 MONARCH_END
 
+double float_arg(PyObject* o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw python_error();
+    return v;
+}
+std::vector<Tensor> tensors_arg(PyObject* o, const char* name)
+{
+    std::vector<Tensor> r;
+    if (o == Py_None) return r;
+    TORCH_CHECK_TYPE(PyList_Check(o) || PyTuple_Check(o), name, " must be a list of tensors, got ", Py_TYPE(o)->tp_name);
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+    for (Py_ssize_t i = 0; i < n; ++i) r.push_back(tensor_arg(PySequence_Fast_GET_ITEM(o, i), name));
+    return r;
+}
+// three numbers, how many steps, what the norm gets added
+Steps steps_arg(PyObject* coefficients, PyObject* steps, PyObject* eps)
+{
+    TORCH_CHECK_TYPE((PyList_Check(coefficients) || PyTuple_Check(coefficients)) && PySequence_Fast_GET_SIZE(coefficients) == 3,
+                     "coefficients must be three numbers");
+    Steps k;
+    for (int i = 0; i < 3; ++i) k.c[i] = (float)float_arg(PySequence_Fast_GET_ITEM(coefficients, i));
+    const int64_t n = int_arg(steps);
+    TORCH_CHECK_VALUE(n >= 1 && n <= 1000, "steps must be from 1 to 1000, got ", n);
+    k.steps = (int)n;
+    k.eps = (float)float_arg(eps);
+    return k;
+}
+
+// orthogonalize(G, X, coefficients, steps, eps, workspace, stream)
+MONARCH_CALL(py_orthogonalize, 7)
+    const Tensor G = tensor_arg(a[0], "G"), X = optional_arg(a[1], "X"), ws = optional_arg(a[5], "workspace");
+    const Steps k = steps_arg(a[2], a[3], a[4]);
+    const StreamArg st = stream_arg(a[6]);
+    return THPVariable_Wrap(unlocked([&] { return orthogonalize(G, X, k, ws, st); }));
+MONARCH_END
+
+// muon_step(weights, grads, momenta, masters, lr, momentum, decay, scale, nesterov, coefficients, steps, eps, workspace, stream)
+MONARCH_CALL(py_muon_step, 14)
+    const MuonTensors t{tensors_arg(a[0], "weights"), tensors_arg(a[1], "grads"), tensors_arg(a[2], "momenta"), tensors_arg(a[3], "masters")};
+    const MuonNumbers r{(float)float_arg(a[4]), (float)float_arg(a[5]), (float)float_arg(a[6]), (float)float_arg(a[7]), bool_arg(a[8])};
+    const Steps k = steps_arg(a[9], a[10], a[11]);
+    const Tensor ws = optional_arg(a[12], "workspace");
+    const StreamArg st = stream_arg(a[13]);
+    unlocked([&] {
+        muon_step(t, r, k, ws, st);
+        return 0;
+    });
+    Py_RETURN_NONE;
+MONARCH_END
+
 PyObject* py_set_error(PyObject*, PyObject* cls)
 {
     Py_INCREF(cls);
@@ -833,7 +976,8 @@ PyMethodDef g_methods[] = {
     MONARCH_ENTRY(fwd), MONARCH_ENTRY(fwd_static), MONARCH_ENTRY(fwd_ws), MONARCH_ENTRY(fwd_bias), MONARCH_ENTRY(fwd_bias_gelu),
     MONARCH_ENTRY(fwd_t), MONARCH_ENTRY(fwd_save), MONARCH_ENTRY(bwd), MONARCH_ENTRY(to_dense), MONARCH_ENTRY(c64_apply),
     MONARCH_ENTRY(c64_bwd), MONARCH_ENTRY(project), MONARCH_ENTRY(linear),
-    MONARCH_ENTRY(xent_fwd), MONARCH_ENTRY(xent_bwd), MONARCH_ENTRY(xent_total), MONARCH_ENTRY(vocab_loss), {"set_error", py_set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    MONARCH_ENTRY(xent_fwd), MONARCH_ENTRY(xent_bwd), MONARCH_ENTRY(xent_total), MONARCH_ENTRY(vocab_loss),
+    MONARCH_ENTRY(orthogonalize), MONARCH_ENTRY(muon_step), {"set_error", py_set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

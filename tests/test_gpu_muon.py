@@ -1,0 +1,216 @@
+"""Orthogonalised updates, and the optimiser's step built on them, against their definition in 64 bits.
+
+Bounds: fp32 results are held to the 1e-5 of the norm that every fp32 result of the library is held to (operands of 22 bits, three a step,
+2^-23 each, that five steps let grow a few times: about 1e-6); results in bf16 to one rounding, 2^-8.  Where few singular values hold the
+whole matrix, the rounding of the large ones grows like small singular values do: 3.4445^5 = 485 times."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+MUON = (3.4445, -4.7750, 2.0315)
+CUBIC = (1.5, -0.5, 0.0)
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+BOUND = {"f32": 1e-5, "bf16": 2.0 ** -8}
+# blocks, m, n: one number, rows, columns, the tiles' edges, both ways round, odd sizes, more blocks than CUs
+SHAPES = [(1, 1, 1), (1, 1, 9), (3, 5, 2), (16, 16, 16), (4, 33, 20), (5, 32, 48), (64, 64, 64), (2, 65, 64), (3, 20, 150), (2, 130, 70), (1, 96, 300),
+          (3, 192, 192), (2, 256, 100), (1, 300, 257), (300, 24, 40), (9, 128, 512)]
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2204_00595_amd import binding as b
+    return b
+
+
+def gradient(shape, dtype, seed=0, size=1e-3):
+    gen = torch.Generator().manual_seed(seed + sum(shape))
+    return (torch.randn(shape, generator=gen) * size).to(DTYPES[dtype])
+
+
+def orthogonal(G, steps=5, c=MUON, eps=1e-7):
+    X = G.double()
+    X = X / (X.square().sum((-2, -1), keepdim=True).sqrt() + eps)
+    tall = X.shape[-2] > X.shape[-1]
+    X = X.transpose(-2, -1) if tall else X
+    for _ in range(steps):
+        A = X @ X.transpose(-2, -1)
+        X = c[0] * X + (c[1] * A + c[2] * A @ A) @ X
+    return X.transpose(-2, -1) if tall else X
+
+
+def far(got, want):
+    got = got.double().cpu()
+    assert torch.isfinite(got).all()
+    d, norm = (got - want).norm().item(), want.norm().item()
+    return d / norm if norm else d
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_orthogonalize(binding, shape, dtype):
+    G = gradient(shape, dtype)
+    X = binding.monarch_orthogonalize(G.cuda())
+    assert X.dtype == G.dtype and X.shape == G.shape
+    assert far(X, orthogonal(G)) <= BOUND[dtype]
+    assert torch.equal(X, binding.monarch_orthogonalize(G.cuda()))
+
+
+@pytest.mark.parametrize("shape", [(3, 40, 64), (2, 200, 90)])
+@pytest.mark.parametrize("steps, c", [(1, MUON), (2, MUON), (4, MUON), (7, MUON), (10, CUBIC)])
+def test_steps_and_coefficients(binding, shape, steps, c):
+    G = gradient(shape, "f32")
+    assert far(binding.monarch_orthogonalize(G.cuda(), steps=steps, coefficients=c), orthogonal(G, steps, c)) <= BOUND["f32"]
+
+
+def test_what_it_is_for(binding):
+    """Singular values between 0.65 and 1.25 where those of the block were not below a hundredth of its norm; the cubic polynomial, in many steps,
+    gives the orthogonal factor."""
+    G = gradient((4, 96, 160), "f32")
+    s = torch.linalg.svdvals(binding.monarch_orthogonalize(G.cuda()).double().cpu())
+    assert 0.65 <= s.min() and s.max() <= 1.25
+    U, _, Vh = torch.linalg.svd(G.double(), full_matrices=False)
+    assert far(binding.monarch_orthogonalize(G.cuda(), steps=30, coefficients=CUBIC), U @ Vh) <= BOUND["f32"]
+
+
+def test_a_matrix_is_a_stack_of_one(binding):
+    G = gradient((70, 110), "f32").cuda()
+    assert torch.equal(binding.monarch_orthogonalize(G), binding.monarch_orthogonalize(G[None])[0])
+
+
+@pytest.mark.parametrize("shape", [(4, 24, 40), (3, 150, 90)])
+def test_blocks_do_not_touch_one_another(binding, shape):
+    G = gradient(shape, "f32")
+    alone = binding.monarch_orthogonalize(G.cuda())
+    G[0] = 0
+    G[1, 3, 2] = float("nan")
+    X = binding.monarch_orthogonalize(G.cuda())
+    assert (X[0] == 0).all() and not torch.isfinite(X[1]).all() and torch.equal(X[2:], alone[2:])
+    G[1, 3, 2] = float("-inf")
+    X = binding.monarch_orthogonalize(G.cuda())
+    assert (X[0] == 0).all() and not torch.isfinite(X[1]).all() and torch.equal(X[2:], alone[2:])
+
+
+@pytest.mark.parametrize("shape", [(2, 30, 50), (2, 140, 70)])
+@pytest.mark.parametrize("size", [1e-36, 1e-20, 1e20, 1e36])
+def test_any_magnitude(binding, shape, size):
+    G = gradient(shape, "f32", size=size)
+    assert far(binding.monarch_orthogonalize(G.cuda(), eps=0.0), orthogonal(G, eps=0.0)) <= BOUND["f32"]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m, n", [(48, 32), (100, 260)])
+def test_few_directions(binding, m, n, dtype):
+    gen = torch.Generator().manual_seed(5)
+    G = (torch.randn((2, m, 1), generator=gen) @ torch.randn((2, 1, n), generator=gen)).to(DTYPES[dtype])
+    G[1] = 0.01
+    grown = 485 * 2.0 ** -20
+    assert far(binding.monarch_orthogonalize(G.cuda()), orthogonal(G)) <= grown + (BOUND["bf16"] if dtype == "bf16" else 0)
+
+
+def reference(weights, grads, momenta, lr, momentum, decay, nesterov, scale, masters=None):
+    out = []
+    for w, g, v, k in zip(weights, grads, momenta, masters or weights):
+        v = momentum * v.double() + g.double()
+        u = g.double() + momentum * v if nesterov else v
+        new = (1 - lr * decay) * k.double() - lr * scale * orthogonal(u)
+        out.append((new, v))
+    return out
+
+
+@pytest.mark.parametrize("kind", ["f32", "f32 weights, bf16 gradients", "bf16", "masters"])
+@pytest.mark.parametrize("count, shape", [(1, (4, 48, 48)), (3, (2, 100, 40)), (5, (4, 64, 192)), (2, (130, 70)), (50, (2, 6, 9))])
+def test_muon_step(binding, count, shape, kind):
+    nesterov, lr, decay = count != 3, 0.02, 0.1
+    wt = torch.float32 if kind.startswith("f32") else torch.bfloat16
+    gt = torch.float32 if kind == "f32" else torch.bfloat16
+    kept = [gradient(shape, "f32", 100 + i, 0.2) for i in range(count)]
+    weights = [w.to(wt) for w in kept]
+    grads = [gradient(shape, "f32", 200 + i).to(gt) for i in range(count)]
+    momenta = [gradient(shape, "f32", 300 + i, 5e-3) for i in range(count)]
+    masters = kept if kind == "masters" else None
+    scale = max(1.0, shape[-2] / shape[-1]) ** 0.5
+    want = reference(weights, grads, momenta, lr, 0.9, decay, nesterov, scale, masters)
+    wd, gd, vd = ([t.cuda() for t in ts] for ts in (weights, grads, momenta))
+    kd = [t.cuda() for t in masters] if masters else None
+    assert binding.monarch_muon_step(wd, gd, vd, lr=lr, momentum=0.9, weight_decay=decay, nesterov=nesterov, masters=kd) is None
+    for i, (w, v) in enumerate(want):
+        assert far(vd[i], v) <= 1e-6
+        assert torch.equal(gd[i].cpu(), grads[i])
+        if masters:
+            assert far(kd[i], w) <= 1e-6
+            assert torch.equal(wd[i], kd[i].bfloat16())
+        else:
+            assert far(wd[i], w) <= (1e-6 if wt == torch.float32 else 2.0 ** -8)
+
+
+def test_muon_step_moves_by_its_scale(binding):
+    w, g, v = (gradient((3, 40, 30), "f32", i).cuda() for i in range(3))
+    X = binding.monarch_orthogonalize(g)
+    for scale in (0.2, 3.0):
+        wd, vd = w.clone(), torch.zeros_like(v)
+        binding.monarch_muon_step([wd], [g], [vd], lr=0.5, momentum=0.0, scale=scale)
+        assert far(wd, (w.double() - 0.5 * scale * X.double()).cpu()) <= 1e-6 and torch.equal(vd, g)
+
+
+def test_on_another_stream_and_in_a_graph(binding):
+    G = gradient((4, 100, 150), "f32").cuda()
+    want = binding.monarch_orthogonalize(G)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    X = binding.monarch_orthogonalize(G, stream=side)
+    side.synchronize()
+    assert torch.equal(X, want)
+    small = gradient((16, 16, 16), "f32").cuda()
+    want_small = binding.monarch_orthogonalize(small)
+    w, v = torch.zeros_like(G), torch.zeros_like(G)
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            X, Y = binding.monarch_orthogonalize(G), binding.monarch_orthogonalize(small)
+            binding.monarch_muon_step([w], [G], [v], lr=1.0, momentum=0.0)
+    for k in range(1, 4):
+        X.fill_(3)
+        Y.fill_(3)
+        (torch.randn(300, 1000, device="cuda") @ torch.randn(1000, 50, device="cuda")).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(X, want) and torch.equal(Y, want_small) and torch.equal(v, G)
+        assert far(w, -k * want.double().cpu()) <= 1e-6
+
+
+def test_nothing_to_do(binding):
+    assert binding.monarch_orthogonalize(torch.empty((0, 8, 8), device="cuda")).shape == (0, 8, 8)
+    assert binding.monarch_muon_step([], [], [], lr=0.1) is None
+
+
+def test_refusals(binding):
+    G = gradient((2, 8, 8), "f32").cuda()
+    for bad in (G.half(), G.double(), G.long()):
+        with pytest.raises(TypeError):
+            binding.monarch_orthogonalize(bad)
+    for bad in (G[0, 0], G[None], G.transpose(1, 2), G.cpu()):
+        with pytest.raises(ValueError):
+            binding.monarch_orthogonalize(bad)
+    with pytest.raises(ValueError):
+        binding.monarch_orthogonalize(G, steps=0)
+    with pytest.raises(TypeError):
+        binding.monarch_orthogonalize(G, coefficients=(1.0, 2.0))
+    with pytest.raises(binding.MonarchError):
+        binding.monarch_orthogonalize(G, coefficients=(90.0, -10.0, 1.0))
+    with pytest.raises(binding.MonarchError):
+        binding.monarch_orthogonalize(G, eps=-1.0)
+    with pytest.raises(binding.MonarchError):
+        binding.monarch_orthogonalize(G, eps=math.nan)
+    with pytest.raises(ValueError):
+        binding.monarch_muon_step([G], [G, G], [G], lr=0.1)
+    with pytest.raises(ValueError):
+        binding.monarch_muon_step([G, G], [G, G], [G, G[:, :4].contiguous()], lr=0.1)
+    with pytest.raises(TypeError):
+        binding.monarch_muon_step([G], [G], [G.bfloat16()], lr=0.1)
+    with pytest.raises(TypeError):
+        binding.monarch_muon_step([G.clone()], [G], [G.clone()], lr=0.1, masters=[G.clone()])   # masters of fp32 weights
+    with pytest.raises(TypeError):
+        binding.monarch_muon_step(G, [G], [G], lr=0.1)

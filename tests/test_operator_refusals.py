@@ -71,3 +71,59 @@ def test_loss_total(binding):
     assert L.monarch_xent_total(P, P, None, 3, -100, 1, None) == binding.MONARCH_ERR_INVALID
     assert L.monarch_xent_total(None, P, P, 3, -100, 1, None) == binding.MONARCH_ERR_INVALID
     assert L.monarch_xent_total(P, P, P, -3, -100, 1, None) == binding.MONARCH_ERR_INVALID
+
+
+def _floats(*v):
+    import ctypes
+    return (ctypes.c_float * len(v))(*v)
+
+
+def _pointers(*v):
+    import ctypes
+    return (ctypes.c_void_p * len(v))(*v)
+
+
+MUON = (3.4445, -4.7750, 2.0315)
+
+
+def test_orthogonalize(binding):
+    L = binding.lib()
+    need = binding.monarch_orthogonalize_workspace_bytes(3, 20, 30, 0)
+    assert need > 0
+    assert binding.monarch_orthogonalize_workspace_bytes(3, 20, 30, 9) == 0
+
+    def call(G=P, X=P, blocks=3, m=20, n=30, c=_floats(*MUON), steps=5, eps=1e-7, dtype=0, ws=P, ws_bytes=need):
+        return L.monarch_orthogonalize(G, X, blocks, m, n, c, steps, eps, dtype, None, ws, ws_bytes)
+
+    assert call(blocks=0) == binding.MONARCH_OK
+    assert call(blocks=0, G=None, X=None, ws=None) == binding.MONARCH_OK
+    for bad in (dict(G=None), dict(X=None), dict(G=P + 4), dict(X=P + 8), dict(blocks=-1), dict(m=0), dict(n=-2), dict(dtype=4), dict(c=None),
+                dict(steps=0), dict(eps=-1e-3), dict(eps=float("nan")), dict(c=_floats(60.0, -30.0, 1.0)), dict(c=_floats(1.0, float("nan"), 0.0))):
+        assert call(**bad) == binding.MONARCH_ERR_INVALID, bad
+    for bad in (dict(ws=None), dict(ws=P + 128), dict(ws_bytes=need - 1)):
+        assert call(**bad) == binding.MONARCH_ERR_WORKSPACE, bad
+    for bad in (dict(m=(1 << 14) + 1), dict(n=(1 << 14) + 1), dict(blocks=65536)):
+        assert call(**bad) == binding.MONARCH_ERR_UNSUPPORTED, bad
+
+
+def test_muon_step(binding):
+    L = binding.lib()
+    need = binding.monarch_muon_step_workspace_bytes(2, 3, 20, 30, 1, True)
+    assert need > 0
+    assert binding.monarch_muon_step_workspace_bytes(2, 3, 20, 30, 0, True) == 0     # masters of fp32 weights
+    # no more than the tensors of one launch at a time
+    assert binding.monarch_muon_step_workspace_bytes(1000, 3, 20, 30, 1) == binding.monarch_muon_step_workspace_bytes(48, 3, 20, 30, 1)
+    two = _pointers(P, P)
+
+    def call(count=2, w=two, g=two, v=two, k=None, blocks=3, m=20, n=30, c=_floats(*MUON), steps=5, eps=1e-7, dtype=1, gdtype=0, ws=P, ws_bytes=need):
+        return L.monarch_muon_step(count, w, g, v, k, blocks, m, n, 0.1, 0.9, 0.0, 1.0, 1, c, steps, eps, dtype, gdtype, None, ws, ws_bytes)
+
+    assert call(count=0) == binding.MONARCH_OK
+    assert call(blocks=0, w=None) == binding.MONARCH_OK
+    for bad in (dict(count=-1), dict(w=None), dict(g=None), dict(v=None), dict(w=_pointers(P, None)), dict(g=_pointers(P, P + 2)),
+                dict(v=_pointers(P + 4, P)), dict(k=_pointers(P, None)), dict(k=two, dtype=0), dict(gdtype=3), dict(dtype=2), dict(m=-1), dict(steps=-1),
+                dict(c=_floats(101.0, 0.0, 0.0))):
+        assert call(**bad) == binding.MONARCH_ERR_INVALID, bad
+    for bad in (dict(ws=None), dict(ws=P + 1), dict(ws_bytes=100)):
+        assert call(**bad) == binding.MONARCH_ERR_WORKSPACE, bad
+    assert call(blocks=70000) == binding.MONARCH_ERR_UNSUPPORTED

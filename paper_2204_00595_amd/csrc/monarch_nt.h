@@ -83,7 +83,7 @@ __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const
     const int r16 = lane & 15, at0 = 16 * ((lane >> 4) ^ (lane & 7)), at1 = at0 ^ 64;
     const unsigned char* fa = lds + (C::row0() + r16) * 128;
     const unsigned char* fb = lds + C::BM * 128 + (C::col0() + r16) * 128;
-    ask(step0, 0);
+    if (steps > 0) ask(step0, 0);
     for (int s = 0; s < steps; ++s) {
         const int buffer = s & 1;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -113,6 +113,17 @@ __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const
         }
     }
 #endif
+}
+
+// Among four lanes (4q .. 4q + 3) with four 16-bit numbers each: lane i gets number i of all four.
+__device__ __forceinline__ u32x2 change_places(u32x2 v)
+{
+    const int lane = threadIdx.x;
+    const uint32_t a = v[0], b = v[1];
+    const uint32_t oa = __builtin_amdgcn_mov_dpp((int)a, 0xB1, 0xF, 0xF, true), ob = __builtin_amdgcn_mov_dpp((int)b, 0xB1, 0xF, 0xF, true);
+    const uint32_t c = lane & 1 ? pick_hi16(oa, a) : pick_lo16(a, oa), d = lane & 1 ? pick_hi16(ob, b) : pick_lo16(b, ob);
+    const uint32_t oc = __builtin_amdgcn_mov_dpp((int)c, 0x4E, 0xF, 0xF, true), od = __builtin_amdgcn_mov_dpp((int)d, 0x4E, 0xF, 0xF, true);
+    return lane & 2 ? u32x2{od, d} : u32x2{c, oc};
 }
 
 // Tile of a workgroup: the eight XCDs take workgroups in turn, and each gets a run of tiles that lie together (groups of 8 tiles along m, n

@@ -38,17 +38,6 @@ __device__ __forceinline__ u32x2 take_plane(f32x4& v)
     }
     return u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
 }
-// Among four lanes (4q .. 4q + 3) with four 16-bit numbers each: lane i gets number i of all four.
-__device__ __forceinline__ u32x2 change_places(u32x2 v)
-{
-    const int lane = threadIdx.x;
-    const uint32_t a = v[0], b = v[1];
-    const uint32_t oa = __builtin_amdgcn_mov_dpp((int)a, 0xB1, 0xF, 0xF, true), ob = __builtin_amdgcn_mov_dpp((int)b, 0xB1, 0xF, 0xF, true);
-    const uint32_t c = lane & 1 ? pick_hi16(oa, a) : pick_lo16(a, oa), d = lane & 1 ? pick_hi16(ob, b) : pick_lo16(b, ob);
-    const uint32_t oc = __builtin_amdgcn_mov_dpp((int)c, 0x4E, 0xF, 0xF, true), od = __builtin_amdgcn_mov_dpp((int)d, 0x4E, 0xF, 0xF, true);
-    return lane & 2 ? u32x2{od, d} : u32x2{c, oc};
-}
-
 // ---- norm, momentum, first operands ----
 
 constexpr int kChunk = 4096;  // numbers of a block that a workgroup adds up

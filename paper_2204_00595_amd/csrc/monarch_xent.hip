@@ -4,8 +4,10 @@
 // and holds G for a piece of the vocabulary.
 //
 // Every product is along the rows of its operands (monarch_nt.h), so what a product contracts over lies last: dx takes W^T, dW takes x^T
-// and G^T, laid out here.  fp32 operands are two binary16 planes: 22 bits of each number at three matrix products instead of the six
-// that three bf16 planes need; powers of two, one for each row that is not contracted over, keep them in binary16's range.
+// and G^T, laid out here.  The logits take bf16 operands as they are and fp32 operands as two binary16 planes: 22 bits of each number at
+// three matrix products instead of the six that three bf16 planes need; powers of two, one for each row that is not contracted over, keep
+// them in binary16's range.  G, W^T and x^T are binary16 times a power of two for both types, one plane beside bf16 tensors (whose 8 bits
+// fit it whole, so that G keeps 11 bits where bf16 would leave 8) and two beside fp32 ones.
 #include "monarch_xent.h"
 #include "monarch_device.h"
 #include "monarch_nt.h"
@@ -53,97 +55,122 @@ __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 
 // ---- operands ----
 
-// Rows of x or W as an operand: one wave a row.  bf16: copied, zeros up to whole steps.  fp32: two planes, the row's inverse power of two
-// in inv[row], its largest magnitude in top[row].
-template <typename T>
-__global__ __launch_bounds__(256) void pack_rows_kernel(const T* __restrict__ src, int64_t rows, int width, uint16_t* __restrict__ dst,
-                                                        uint32_t row_half, float* __restrict__ inv, float* __restrict__ top)
+constexpr int kTops = 1024;  // workgroups, at most, that leave the largest magnitude they met
+
+// Largest finite magnitude of `n` values (a workgroup of 256).
+__device__ __forceinline__ float largest_of(const float* __restrict__ v, int n)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const T* s = src + row * width;
-    uint16_t* d = dst + row * (int64_t)row_half;
-    if constexpr (sizeof(T) == 2) {
-        for (uint32_t k = lane; k < row_half; k += 64) d[k] = k < (uint32_t)width ? s[k] : (uint16_t)0;
-    } else {
-        float m = 0.f;
-        for (int k = lane; k < width; k += 64) m = fmaxf(m, finite_magnitude(s[k]));
-        m = wave_all(m, max_of);
-        const float up = scale_for(m);
-        if (lane == 0) {
-            inv[row] = inverse_power(up);
-            top[row] = m;
-        }
-        for (uint32_t k = lane; k < row_half / 2; k += 64) {
-            uint16_t hi = 0, lo = 0;
-            if (k < (uint32_t)width) split2(s[k] * up, hi, lo);
-            uint16_t* at = d + (k >> 5) * 64 + (k & 31);
-            at[0] = hi;
-            at[32] = lo;
-        }
-    }
+    __shared__ float part[4];
+    float m = 0.f;
+    for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, v[i]);
+    m = wave_all(m, max_of);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+    return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
 }
 
-// Columns of src (rows x width) as rows of an operand, 64 x 64 at a time.  `dl` (may be null): rows with dl = 0 count as zeros, whatever they
-// hold.  fp32: scaled by the power of two for *top.
+// A wave a row: the largest magnitude of the rows with dl != 0 (dl may be null: all) -> tops[workgroup].  With `dst`, the rows as an operand too.
+// bf16: copied, zeros up to whole steps.  fp32: two planes, the row's inverse power of two in inv[row].
 template <typename T>
-__global__ __launch_bounds__(256) void pack_columns_kernel(const T* __restrict__ src, int64_t rows, int width, uint16_t* __restrict__ dst,
-                                                           uint32_t row_half, const float* __restrict__ dl, const float* __restrict__ top)
+__global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, int64_t rows, int width, uint16_t* __restrict__ dst,
+                                                   uint32_t row_half, float* __restrict__ inv, const float* __restrict__ dl,
+                                                   float* __restrict__ tops)
+{
+    __shared__ float part[4];
+    const int lane = threadIdx.x & 63;
+    float all = 0.f;
+    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * 4) {
+        const T* s = src + row * width;
+        float m = 0.f;
+        if (sizeof(T) == 2 && (width & 7) == 0) {
+            for (int k = lane * 8; k < width; k += 512) {
+                const u32x4 u = ldg128(s + k);
+                uint32_t t = 0;  // (magnitudes of bf16 numbers are in the order of their bits)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t h = (u[e >> 1] >> (16 * (e & 1))) & 0x7fffu;
+                    t = h < 0x7f80u && h > t ? h : t;
+                }
+                m = fmaxf(m, __uint_as_float(t << 16));
+            }
+        } else {
+            for (int k = lane; k < width; k += 64) m = fmaxf(m, finite_magnitude(Elem<T>::load(s + k)));
+        }
+        m = wave_all(m, max_of);
+        if (!(dl && dl[row] == 0.f)) all = fmaxf(all, m);
+        if (!dst) continue;
+        uint16_t* d = dst + row * (int64_t)row_half;
+        if constexpr (sizeof(T) == 2) {
+            for (uint32_t k = lane; k < row_half; k += 64) d[k] = k < (uint32_t)width ? s[k] : (uint16_t)0;
+        } else {
+            const float up = scale_for(m);
+            if (lane == 0) inv[row] = inverse_power(up);
+            for (uint32_t k = lane; k < row_half / 2; k += 64) {
+                uint16_t hi = 0, lo = 0;
+                if (k < (uint32_t)width) split2(s[k] * up, hi, lo);
+                uint16_t* at = d + (k >> 5) * 64 + (k & 31);
+                at[0] = hi;
+                at[32] = lo;
+            }
+        }
+    }
+    if (!tops) return;
+    if (lane == 0) part[threadIdx.x >> 6] = all;
+    __syncthreads();
+    if (threadIdx.x == 0) tops[blockIdx.x] = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+}
+
+// Columns of src (rows x width) as rows of an operand of binary16 planes, 64 x 64 at a time, times the power of two for the largest of
+// tops[0 .. n_tops), which goes to *top.  `dl` (may be null): rows with dl = 0 count as zeros, whatever they hold.
+template <typename T>
+__global__ __launch_bounds__(256) void columns_kernel(const T* __restrict__ src, int64_t rows, int width, uint16_t* __restrict__ dst,
+                                                      uint32_t row_half, const float* __restrict__ dl, const float* __restrict__ tops, int n_tops,
+                                                      float* __restrict__ top)
 {
     constexpr bool kPlanes = sizeof(T) == 4;
-    __shared__ T tile[64][sizeof(T) == 2 ? 66 : 65];
+    __shared__ float tile[64][65];
     const int tid = threadIdx.x;
+    const float largest = largest_of(tops, n_tops), up = scale_for(largest);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) *top = largest;
     const int64_t k0 = (int64_t)blockIdx.x * 64;
     const int c0 = blockIdx.y * 64;
+    if (sizeof(T) == 2 && (width & 7) == 0) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = i * 4 + (tid >> 6), c = tid & 63;
-        T v = 0;
-        if (k0 + r < rows && c0 + c < width && !(dl && dl[k0 + r] == 0.f)) v = src[(k0 + r) * width + c0 + c];
-        tile[r][c] = v;
+        for (int i = 0; i < 2; ++i) {
+            const int r = i * 32 + (tid >> 3), c = (tid & 7) * 8;
+            u32x4 u = {0, 0, 0, 0};
+            if (k0 + r < rows && c0 + c < width && !(dl && dl[k0 + r] == 0.f)) u = ldg128(src + (k0 + r) * width + c0 + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) tile[r][c + e] = __uint_as_float(e & 1 ? u[e >> 1] & 0xffff0000u : u[e >> 1] << 16);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = i * 4 + (tid >> 6), c = tid & 63;
+            float v = 0.f;
+            if (k0 + r < rows && c0 + c < width && !(dl && dl[k0 + r] == 0.f)) v = Elem<T>::load(src + (k0 + r) * width + c0 + c);
+            tile[r][c] = v;
+        }
     }
     __syncthreads();
-    float up = 1.f;
-    if constexpr (kPlanes) up = scale_for(*top);
     // eight along k of one column a piece
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int piece = i * 256 + tid, c = piece >> 3, r = (piece & 7) * 8;
-        if (c0 + c >= width) continue;
         const int64_t k = k0 + r;
-        uint16_t hi[8], lo[8];
+        if (c0 + c >= width || k * (kPlanes ? 2 : 1) >= (int64_t)row_half) continue;
+        uint32_t hi[8], lo[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if constexpr (kPlanes) split2(tile[r + e][c] * up, hi[e], lo[e]);
-            else hi[e] = tile[r + e][c];
+            uint16_t h, l;
+            split2(tile[r + e][c] * up, h, l);
+            hi[e] = h;
+            lo[e] = l;
         }
-        uint16_t* d = dst + (int64_t)(c0 + c) * row_half;
-        if constexpr (kPlanes) {
-            uint16_t* at = d + (k >> 5) * 64 + (k & 31);
-            if (k * 2 < (int64_t)row_half) {
-                *reinterpret_cast<u32x4*>(at) = *reinterpret_cast<const u32x4*>(hi);
-                *reinterpret_cast<u32x4*>(at + 32) = *reinterpret_cast<const u32x4*>(lo);
-            }
-        } else if (k < (int64_t)row_half) {
-            *reinterpret_cast<u32x4*>(d + k) = *reinterpret_cast<const u32x4*>(hi);
-        }
-    }
-}
-
-// largest of n values (one workgroup)
-__global__ __launch_bounds__(1024) void largest_kernel(const float* __restrict__ v, int64_t n, const float* __restrict__ dl, float* __restrict__ out)
-{
-    __shared__ float part[16];
-    float m = 0.f;
-    for (int64_t i = threadIdx.x; i < n; i += 1024)
-        if (!dl || dl[i] != 0.f) m = fmaxf(m, v[i]);
-    m = wave_all(m, max_of);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 16; ++i) m = fmaxf(m, part[i]);
-        *out = m;
+        uint16_t* at = dst + (int64_t)(c0 + c) * row_half + (kPlanes ? (k >> 5) * 64 + (k & 31) : k);
+        *reinterpret_cast<u32x4*>(at) = u32x4{hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16};
+        if constexpr (kPlanes)
+            *reinterpret_cast<u32x4*>(at + 32) = u32x4{lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16};
     }
 }
 
@@ -290,8 +317,11 @@ __global__ __launch_bounds__(1024) void xent_upstream_kernel(const float* __rest
     }
 }
 
-// G of a piece of the vocabulary, once with the vocabulary last (g: rows of the piece's entries) and once with the rows of x last (gt), as
-// operands; both leave by way of LDS in runs of 64 bytes and more.  Entries and rows that do not exist are written as zeros.
+constexpr float kG = 0x1p14f;  // what exp(l - lse) - [v = target] is stored times where the upstream gradient is left out
+
+// G of a piece of the vocabulary as operands of binary16 planes: once with the vocabulary last and without the upstream gradient, which dx
+// takes row by row (g), and once with the rows of x last and with it, times the power of two for the largest one (gt).  Both leave by
+// way of LDS in runs of 64 bytes and more.  Entries and rows that do not exist are written as zeros.
 template <typename C>
 __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const float* __restrict__ lse, const float* __restrict__ dl,
                                                                const float* __restrict__ dl_top, uint16_t* __restrict__ g, uint32_t g_half,
@@ -306,13 +336,14 @@ __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const f
     const int tid = threadIdx.x, lane = tid & 63;
     const int vr = C::row0() + 4 * (lane >> 4), tc = C::col0() + (lane & 15);
     const int64_t left = p.vocab - v0 - vr;
-    float up = 1.f;
-    if constexpr (C::PL == 2) up = scale_for(*dl_top);
+    const float up = scale_for(*dl_top);
+    float d[C::TJ];
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j) {
         const int64_t t = t0 + tc + 16 * j;
         const bool row = t < p.rows;
-        const float ls = row ? lse[t] : 0.f, d = row ? dl[t] * up : 0.f;
+        const float ls = row ? lse[t] : 0.f;
+        d[j] = row ? dl[t] * up : 0.f;
         const int64_t at = row ? p.target[t] - v0 - vr : -1;
 #pragma unroll
         for (int i = 0; i < C::TI; ++i)
@@ -320,38 +351,31 @@ __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const f
             for (int e = 0; e < 4; ++e) {
                 float s = exp2_fast((acc[i][j][e] - ls) * kLog2e);
                 if (at == 16 * i + e) s -= 1.f;
-                acc[i][j][e] = d == 0.f || 16 * i + e >= left ? 0.f : s * d;
+                acc[i][j][e] = d[j] == 0.f || 16 * i + e >= left ? 0.f : s;
             }
     }
+    // plane `plane` of four numbers times `by`
+    auto four = [&](const f32x4& s, float by, int plane) {
+        uint32_t h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float v = s[e] * by;
+            const _Float16 f = (_Float16)v;
+            h[e] = plane ? f32_to_f16_bits(v - (float)f) : (uint32_t)__builtin_bit_cast(uint16_t, f);
+        }
+        return u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+    };
+    // 16-byte piece u of LDS row r in place u ^ (r % 16), of the other way round u ^ (r % 8)
 #pragma unroll
     for (int plane = 0; plane < C::PL; ++plane) {
-        u32x2 v[C::TI][C::TJ];  // four entries of one row of x
-#pragma unroll
-        for (int i = 0; i < C::TI; ++i)
-#pragma unroll
-            for (int j = 0; j < C::TJ; ++j) {
-                if constexpr (C::PL == 1) {
-                    v[i][j] = u32x2{pack_bf16x2(acc[i][j][0], acc[i][j][1]), pack_bf16x2(acc[i][j][2], acc[i][j][3])};
-                } else {
-                    uint32_t h[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const _Float16 f = (_Float16)acc[i][j][e];
-                        h[e] = __builtin_bit_cast(uint16_t, f);
-                        acc[i][j][e] -= (float)f;
-                    }
-                    v[i][j] = u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
-                }
-            }
-        // 16-byte piece u of LDS row r in place u ^ (r % 16)
-        __syncthreads();
         if (g) {
+            __syncthreads();
 #pragma unroll
             for (int i = 0; i < C::TI; ++i)
 #pragma unroll
                 for (int j = 0; j < C::TJ; ++j) {
                     const int r = tc + 16 * j, e = vr + 16 * i;
-                    *reinterpret_cast<u32x2*>(lds + r * (2 * C::BM) + 16 * ((e >> 3) ^ (r & 15)) + 2 * (e & 4)) = v[i][j];
+                    *reinterpret_cast<u32x2*>(lds + r * (2 * C::BM) + 16 * ((e >> 3) ^ (r & 15)) + 2 * (e & 4)) = four(acc[i][j], kG, plane);
                 }
             __syncthreads();
             for (int at = tid; at < C::BN * (C::BM / 8); at += C::THREADS) {
@@ -360,27 +384,16 @@ __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const f
                 uint16_t* to = g + (t0 + r) * (int64_t)g_half + (C::PL == 1 ? k : (k >> 5) * 64 + 32 * plane + (k & 31));
                 *reinterpret_cast<u32x4*>(to) = lds128(lds + r * (2 * C::BM) + 16 * (u ^ (r & 15)));
             }
-            __syncthreads();
         }
         if (!gt) continue;
-        // within four lanes (four rows of x) entries and rows change places
+        __syncthreads();
 #pragma unroll
         for (int i = 0; i < C::TI; ++i)
 #pragma unroll
             for (int j = 0; j < C::TJ; ++j) {
-                const uint32_t a = v[i][j][0], b = v[i][j][1];
-                // with the neighbour: the even lane takes entries 0 and 2 of both rows, the odd lane 1 and 3
-                const uint32_t oa = __builtin_amdgcn_mov_dpp((int)a, 0xB1, 0xF, 0xF, true), ob = __builtin_amdgcn_mov_dpp((int)b, 0xB1, 0xF, 0xF, true);
-                const bool odd = lane & 1;
-                const uint32_t c = odd ? pick_hi16(oa, a) : pick_lo16(a, oa);  // entry 0 (1) of rows 2m, 2m + 1
-                const uint32_t d = odd ? pick_hi16(ob, b) : pick_lo16(b, ob);  // entry 2 (3)
-                // with the lane two on: the lower pair of lanes keeps entries 0 and 1, the upper pair 2 and 3
-                const uint32_t oc = __builtin_amdgcn_mov_dpp((int)c, 0x4E, 0xF, 0xF, true), od = __builtin_amdgcn_mov_dpp((int)d, 0x4E, 0xF, 0xF, true);
-                const bool upper = lane & 2;
-                const u32x2 four = upper ? u32x2{od, d} : u32x2{c, oc};
-                // lane q of the four holds entry (q % 2) + 2 (q / 2) = q of rows 0 .. 3
                 const int r = vr + 16 * i + (lane & 3), e = C::col0() + 16 * j + (lane & 12);
-                *reinterpret_cast<u32x2*>(lds + r * (2 * C::BN) + 16 * ((e >> 3) ^ (r & 7)) + 2 * (e & 4)) = four;
+                *reinterpret_cast<u32x2*>(lds + r * (2 * C::BN) + 16 * ((e >> 3) ^ (r & 7)) + 2 * (e & 4)) =
+                    change_places(four(acc[i][j], d[j], plane));
             }
         __syncthreads();
         for (int at = tid; at < C::BM * (C::BN / 8); at += C::THREADS) {
@@ -392,54 +405,76 @@ __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const f
     }
 }
 
-// out[n][m] (rows of ld) = scale * sum over steps of A[m] B[n] (+ sum[n][m]), as OUT or, with `more`, as a running sum in fp32.
+// What a product of two operands of planes is times: the inverse powers of two of both, and for dx each row's upstream gradient.
+struct Unscale {
+    const float *top_a, *top_b;  // top_b null: kG alone
+    const float* row;            // of the rows of b (may be null)
+    // two factors (their product alone may be out of range)
+    __device__ __forceinline__ f32x2 factors() const
+    {
+        return f32x2{inverse_power(scale_for(*top_a)), top_b ? inverse_power(scale_for(*top_b)) : 1.f / kG};
+    }
+};
+
+// out[n][m] (rows of ld) = what A[m] B[n] add up to over the steps, unscaled, as OUT; or, with `part`, as it is to part[z] (+ what lies
+// there), a share of the steps each.
 template <typename C, typename OUT>
-__global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, NtOperand bn, int tiles_m, int tiles_n, int steps,
-                                                                  OUT* out, int64_t ld, float* sum, int add, int more,
-                                                                  const float* __restrict__ top_a, const float* __restrict__ top_b)
+__global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, NtOperand bn, int tiles_m, int tiles_n, int steps, int shares,
+                                                                  OUT* out, int64_t ld, float* part, int add, Unscale by)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int tm, tn;
-    if (!nt_place(blockIdx.x, tiles_m, tiles_n, tm, tn)) return;
+    // (the shares of a tile follow one another on other XCDs; those of neighbouring tiles lie together)
+    const int tiles8 = (int)gridDim.x / shares, share = (int)blockIdx.x / tiles8;
+    if (!nt_place((int)blockIdx.x - share * tiles8, tiles_m, tiles_n, tm, tn)) return;
+    const int each = (steps + shares - 1) / shares, first = share * each, count = steps - first < each ? steps - first : each;
     f32x4 acc[C::TI][C::TJ];
-    nt_product<C>(am, (int64_t)tm * C::BM, bn, (int64_t)tn * C::BN, 0, steps, lds, acc);
-    float sa = 1.f, sb = 1.f;
-    if constexpr (C::PL == 2) {
-        sa = inverse_power(scale_for(*top_a));
-        sb = inverse_power(scale_for(*top_b));
-    }
+    nt_product<C>(am, (int64_t)tm * C::BM, bn, (int64_t)tn * C::BN, first, count, lds, acc);
     const int lane = threadIdx.x & 63;
     const int64_t m0 = (int64_t)tm * C::BM + C::row0() + 4 * (lane >> 4), n0 = (int64_t)tn * C::BN + C::col0() + (lane & 15);
     const bool whole = (ld & 3) == 0;
+    const f32x2 f = part ? f32x2{1.f, 1.f} : by.factors();
+    float* sum = part ? part + (int64_t)share * bn.rows * ld : nullptr;
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j) {
         const int64_t n = n0 + 16 * j;
         if (n >= bn.rows) continue;
+        const float row = !part && by.row ? by.row[n] : 1.f;
 #pragma unroll
         for (int i = 0; i < C::TI; ++i) {
             const int64_t m = m0 + 16 * i;
             if (m >= am.rows) continue;
             f32x4 v = acc[i][j];
-            if constexpr (C::PL == 2) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = v[e] * sa * sb;
-            }
+            for (int e = 0; e < 4; ++e) v[e] = v[e] * f[0] * f[1] * row;
             const int64_t at = n * ld + m;
             if (whole) {
-                if (add) v += *reinterpret_cast<const f32x4*>(sum + at);
-                if (more) *reinterpret_cast<f32x4*>(sum + at) = v;
+                if (sum) *reinterpret_cast<f32x4*>(sum + at) = add ? v + *reinterpret_cast<const f32x4*>(sum + at) : v;
                 else if constexpr (sizeof(OUT) == 4) *reinterpret_cast<f32x4*>(out + at) = v;
                 else *reinterpret_cast<u32x2*>(out + at) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (m + e >= am.rows) break;
-                    if (add) v[e] += sum[at + e];
-                    if (more) sum[at + e] = v[e];
+                    if (sum) sum[at + e] = add ? v[e] + sum[at + e] : v[e];
                     else Elem<OUT>::store(out + at + e, v[e]);
                 }
             }
         }
+    }
+}
+
+// The shares together, in order: out = unscaled sum of part[0 .. shares).
+template <typename OUT>
+__global__ __launch_bounds__(256) void xent_shares_kernel(const float* __restrict__ part, int shares, int64_t rows, int64_t ld, OUT* __restrict__ out,
+                                                          Unscale by)
+{
+    const int64_t size = rows * ld;
+    const f32x2 f = by.factors();
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
+        float s = part[i];
+        for (int k = 1; k < shares; ++k) s += part[k * size + i];
+        Elem<OUT>::store(out + i, s * f[0] * f[1] * (by.row ? by.row[i / ld] : 1.f));
     }
 }
 
@@ -483,6 +518,8 @@ using Low = NtTile<128, 64, 32, 64, 1, false>;
 using Big2 = NtTile<256, 256, 128, 64, 2, true>;
 using Mid2 = NtTile<128, 128, 64, 64, 2, true>;
 using Low2 = NtTile<128, 64, 32, 64, 2, true>;
+using Big16 = NtTile<256, 256, 128, 64, 1, true>;
+using Mid16 = NtTile<128, 128, 64, 64, 1, true>;
 
 // bytes handed out of a workspace
 struct Area {
@@ -515,7 +552,7 @@ struct Plan {
 
 struct Sides {  // x and W as operands, with their powers of two
     uint16_t *x = nullptr, *w = nullptr;
-    float *xinv = nullptr, *winv = nullptr, *xtop = nullptr, *wtop = nullptr;
+    float *xinv = nullptr, *winv = nullptr;
     void lay(const Plan& p, Area& a)
     {
         if (!p.packs()) return;
@@ -523,9 +560,7 @@ struct Sides {  // x and W as operands, with their powers of two
         w = a.take<uint16_t>((size_t)p.vocab * p.half(p.width));
         if (!p.f32) return;
         xinv = a.take<float>(p.rows);
-        xtop = a.take<float>(p.rows);
         winv = a.take<float>(p.vocab);
-        wtop = a.take<float>(p.vocab);
     }
 };
 
@@ -543,20 +578,53 @@ struct FwdArea {
     }
 };
 
+// How a product of m x n numbers over `steps` steps is run, by an estimate of its time in microseconds on 256 CUs: whole rounds of workgroups, one of
+// 256 x 256 a CU or two of 128 x 128, each over a share of the steps, and the shares' sums written and read.  Measured: a step of 256 x 256
+// takes 1.6 us (two planes 2.2), one of 128 x 128 0.9 (1.2) beside another and 0.55 (0.75) alone.
+struct Cut {
+    bool big;
+    int shares;
+    double us;
+};
+Cut cut_for(int64_t m, int64_t n, int steps, bool planes, int pieces_before)
+{
+    Cut best{false, 1, 1e30};
+    for (int big = 0; big < 2; ++big) {
+        const int64_t side = big ? 256 : 128, tiles = ((m + side - 1) / side) * ((n + side - 1) / side);
+        for (int shares = 1; shares <= 32 && shares * 4 <= (steps > 4 ? steps : 4); shares = shares < 4 ? shares + 1 : shares + shares / 2) {
+            const int64_t groups = tiles * shares, slots = big ? 256 : 512;
+            const bool alone = !big && groups <= 256;
+            const double step = (big ? 1.6 : alone ? 0.55 : 0.9) * (planes ? 1.38 : 1.0);
+            const double mb = m * n * 4e-6 * shares;
+            const double us = (double)((groups + slots - 1) / slots) * ((steps + shares - 1) / shares * step + (big ? 4 : 3)) +
+                              (shares > 1 || pieces_before ? 3 + 2 * mb / 4 : 0);
+            if (us < best.us && mb < 512) best = Cut{big != 0, shares, us};
+        }
+    }
+    return best;
+}
+
 constexpr size_t kPieceBytes = (size_t)1 << 30;  // G of a piece of the vocabulary, both ways round, where the workspace has room for it
 
 struct BwdArea {
     Sides sides;
     uint16_t *wt, *xt, *g, *gt;
-    float *dl, *tops, *sum;  // tops: dl, x, W
-    int piece;               // entries of the vocabulary, whole tiles
+    float *dl, *top, *tops, *dx_part, *dw_part;  // top: largest dl, x, W; tops: of workgroups, x then W
+    int piece;                                   // entries of the vocabulary, whole tiles
+    Cut dx_cut, dw_cut, dw_last;                 // of a whole piece, and of the last one
     uint32_t g_half, gt_half, wt_half, xt_half;
+    int entries_of(const Plan& p, int v0) const { return p.vocab - v0 < piece ? p.vocab - v0 : piece; }
     size_t lay(const Plan& p, char* base, int64_t tiles_of_piece)
     {
         Area a{base};
         sides.lay(p, a);
         const int64_t tokens = p.row_tiles() * p.bt();
         piece = (int)tiles_of_piece * p.bv();
+        const int per = p.per_step(), last = p.vocab % piece ? p.vocab % piece : piece, first = p.vocab < piece ? p.vocab : piece;
+        const bool several = piece < p.vocab;
+        dx_cut = cut_for(p.width, p.rows, (first + per - 1) / per, p.f32, several);
+        dw_cut = cut_for(p.width, first, (int)((p.rows + per - 1) / per), p.f32, 0);
+        dw_last = cut_for(p.width, last, (int)((p.rows + per - 1) / per), p.f32, 0);
         g_half = p.half(piece);
         gt_half = p.half(tokens);
         wt_half = p.half((int64_t)p.parts() * p.bv());
@@ -566,20 +634,22 @@ struct BwdArea {
         g = a.take<uint16_t>((size_t)tokens * g_half);
         gt = a.take<uint16_t>((size_t)piece * gt_half);
         dl = a.take<float>(p.rows);
-        tops = a.take<float>(3);
-        sum = tiles_of_piece < p.parts() && !p.f32 ? a.take<float>((size_t)p.rows * p.width) : nullptr;
+        top = a.take<float>(3);
+        tops = a.take<float>(2 * kTops);
+        dx_part = dx_cut.shares > 1 || several ? a.take<float>((size_t)dx_cut.shares * p.rows * p.width) : nullptr;
+        const size_t one = dw_cut.shares > 1 ? (size_t)dw_cut.shares * first : 0, two = dw_last.shares > 1 ? (size_t)dw_last.shares * last : 0;
+        dw_part = one || two ? a.take<float>((one > two ? one : two) * p.width) : nullptr;
         return a.used;
     }
-    // Pieces of one length each, as few as kPieceBytes and a workspace of `room` bytes allow; 0: not even one tile of the vocabulary fits.
+    // Pieces as long as kPieceBytes and a workspace of `room` bytes allow, a little shorter where the tiles of dW then fill whole rounds; 0: not even
+    // one tile of the vocabulary fits.
     size_t fit(const Plan& p, char* base, size_t room)
     {
-        const int64_t tiles = p.parts(), tokens = p.row_tiles() * p.bt();
+        const int64_t tiles = p.parts(), tokens = p.row_tiles() * p.bt(), across = (p.width + 255) / 256, round = 256 / across * (256 / p.bv());
         int64_t most = (int64_t)(kPieceBytes / ((size_t)tokens * (p.f32 ? 8 : 4))) / p.bv();
         most = most < 1 ? 1 : most > tiles ? tiles : most;
-        for (int64_t pieces = (tiles + most - 1) / most, last = 0; pieces <= tiles; ++pieces) {
-            const int64_t each = (tiles + pieces - 1) / pieces;
-            if (each == last) continue;
-            last = each;
+        for (; most > 0; most = most > 16 ? most - most / 8 : most - 1) {
+            const int64_t each = most < tiles && round > 0 && most >= round ? most / round * round : most;
             const size_t need = lay(p, base, each);
             if (need <= room) return need;
         }
@@ -589,19 +659,25 @@ struct BwdArea {
 
 int launched() { return hip_status(hipGetLastError()); }
 
-int pack_sides(const Plan& p, const Sides& s, const void* x, const void* w, hipStream_t st)
+int rows_grid(int64_t rows) { return (int)((rows + 3) / 4 < kTops ? (rows + 3) / 4 : kTops); }
+// Rows of x (rows) or W (vocab) as an operand, where they do not serve as they are, and (tops) the largest magnitudes.
+template <typename T>
+int run_rows(const void* src, int64_t rows, int width, uint16_t* dst, uint32_t half, float* inv, const float* dl, float* tops, hipStream_t st)
 {
-    if (!p.packs()) return 0;
-    const uint32_t half = p.half(p.width);
-    const dim3 gx((unsigned)((p.rows + 3) / 4)), gw((unsigned)((p.vocab + 3) / 4));
-    if (p.f32) {
-        pack_rows_kernel<float><<<gx, 256, 0, st>>>((const float*)x, p.rows, p.width, s.x, half, s.xinv, s.xtop);
-        pack_rows_kernel<float><<<gw, 256, 0, st>>>((const float*)w, p.vocab, p.width, s.w, half, s.winv, s.wtop);
-    } else {
-        pack_rows_kernel<uint16_t><<<gx, 256, 0, st>>>((const uint16_t*)x, p.rows, p.width, s.x, half, nullptr, nullptr);
-        pack_rows_kernel<uint16_t><<<gw, 256, 0, st>>>((const uint16_t*)w, p.vocab, p.width, s.w, half, nullptr, nullptr);
-    }
+    rows_kernel<T><<<rows_grid(rows), 256, 0, st>>>((const T*)src, rows, width, dst, half, inv, dl, tops);
     return launched();
+}
+int pack_sides(const Plan& p, const Sides& s, const void* x, const void* w, const float* dl, float* tops, hipStream_t st)
+{
+    if (!p.packs() && !tops) return 0;
+    const uint32_t half = p.half(p.width);
+    float* wtops = tops ? tops + kTops : nullptr;
+    if (p.f32) {
+        if (int rc = run_rows<float>(x, p.rows, p.width, s.x, half, s.xinv, dl, tops, st)) return rc;
+        return run_rows<float>(w, p.vocab, p.width, s.w, half, s.winv, nullptr, wtops, st);
+    }
+    if (int rc = run_rows<uint16_t>(x, p.rows, p.width, s.x, half, nullptr, dl, tops, st)) return rc;
+    return run_rows<uint16_t>(w, p.vocab, p.width, s.w, half, nullptr, nullptr, wtops, st);
 }
 
 Logits logits_of(const Plan& p, const Sides& s, const void* x, const void* w, const int64_t* target)
@@ -633,26 +709,36 @@ template <typename C>
 int run_grad(const Logits& l, const float* lse, const BwdArea& a, uint16_t* g, uint16_t* gt, hipStream_t st)
 {
     if (allow_dynamic_lds((const void*)xent_grad_kernel<C>, C::LDS_BYTES) != hipSuccess) return -4;
-    xent_grad_kernel<C><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, lse, a.dl, a.tops, g, a.g_half, gt, a.gt_half);
+    xent_grad_kernel<C><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, lse, a.dl, a.top, g, a.g_half, gt, a.gt_half);
     return launched();
 }
+
+struct Job {  // out (b.rows x a.rows, rows of ld) from operands a and b
+    NtOperand a, b;
+    int steps;
+    void* out;
+    int64_t ld;
+    float* part;  // where the shares go (null: one share, straight to out)
+    bool add, last;
+    Unscale by;
+};
 template <typename C, typename OUT>
-int run_product(const NtOperand& a, const NtOperand& b, int steps, OUT* out, int64_t ld, float* sum, bool add, bool more, const float* top_a,
-                const float* top_b, hipStream_t st)
+int run_product(const Job& j, int shares, hipStream_t st)
 {
     if (allow_dynamic_lds((const void*)xent_product_kernel<C, OUT>, C::LDS_BYTES) != hipSuccess) return -4;
-    const int tm = (int)((a.rows + C::BM - 1) / C::BM), tn = (int)((b.rows + C::BN - 1) / C::BN);
-    xent_product_kernel<C, OUT><<<nt_grid(tm, tn), C::THREADS, C::LDS_BYTES, st>>>(a, b, tm, tn, steps, out, ld, sum, add, more, top_a, top_b);
+    const int tm = (int)((j.a.rows + C::BM - 1) / C::BM), tn = (int)((j.b.rows + C::BN - 1) / C::BN);
+    xent_product_kernel<C, OUT><<<nt_grid(tm, tn) * shares, C::THREADS, C::LDS_BYTES, st>>>(j.a, j.b, tm, tn, j.steps, shares, (OUT*)j.out, j.ld,
+                                                                                            j.part, j.add, j.by);
     return launched();
 }
-// The tile of a product by the number of workgroups: one of 256 x 256 a CU or two of 128 x 128.
 template <typename B, typename M, typename OUT>
-int product(const NtOperand& a, const NtOperand& b, int steps, OUT* out, int64_t ld, float* sum, bool add, bool more, const float* top_a,
-            const float* top_b, hipStream_t st)
+int product(const Job& j, const Cut& cut, hipStream_t st)
 {
-    const int64_t big = ((a.rows + 255) / 256) * ((b.rows + 255) / 256), mid = ((a.rows + 127) / 128) * ((b.rows + 127) / 128);
-    if ((big + 255) / 256 * 4 <= (mid + 511) / 512 * 2) return run_product<B, OUT>(a, b, steps, out, ld, sum, add, more, top_a, top_b, st);
-    return run_product<M, OUT>(a, b, steps, out, ld, sum, add, more, top_a, top_b, st);
+    if (int rc = cut.big ? run_product<B, OUT>(j, cut.shares, st) : run_product<M, OUT>(j, cut.shares, st)) return rc;
+    if (!j.part || !j.last) return 0;
+    const int64_t size = j.b.rows * j.ld, groups = (size + 1023) / 1024;
+    xent_shares_kernel<OUT><<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(j.part, cut.shares, j.b.rows, j.ld, (OUT*)j.out, j.by);
+    return launched();
 }
 
 }  // namespace
@@ -684,7 +770,7 @@ int xent_fwd(const void* x, const void* w, const int64_t* target, float* loss, f
     const Plan p{dtype == 0, rows, vocab, width};
     FwdArea a;
     a.lay(p, (char*)ws);
-    if (int rc = pack_sides(p, a.sides, x, w, st)) return rc;
+    if (int rc = pack_sides(p, a.sides, x, w, nullptr, nullptr, st)) return rc;
     const Logits l = logits_of(p, a.sides, x, w, target);
     const int parts = p.parts(), tile = p.tile();
     int rc;
@@ -701,49 +787,49 @@ int xent_bwd(const void* x, const void* w, const int64_t* target, const float* l
     const Plan p{dtype == 0, rows, vocab, width};
     BwdArea a;
     if (!a.fit(p, (char*)ws, ws_bytes)) return -3;
-    xent_upstream_kernel<<<1, 1024, 0, st>>>(dloss, dloss_stride, divisor, target, ignore, vocab, rows, a.dl, a.tops);
+    xent_upstream_kernel<<<1, 1024, 0, st>>>(dloss, dloss_stride, divisor, target, ignore, vocab, rows, a.dl, a.top);
     if (int rc = launched()) return rc;
-    if (int rc = pack_sides(p, a.sides, x, w, st)) return rc;
-    if (p.f32) {
-        largest_kernel<<<1, 1024, 0, st>>>(a.sides.xtop, rows, a.dl, a.tops + 1);
-        largest_kernel<<<1, 1024, 0, st>>>(a.sides.wtop, vocab, nullptr, a.tops + 2);
-    }
+    if (int rc = pack_sides(p, a.sides, x, w, a.dl, a.tops, st)) return rc;
     const unsigned columns = (unsigned)((width + 63) / 64);
-    auto pack_columns = [&](const void* src, int64_t n, uint16_t* to, uint32_t half, const float* dl, const float* top) {
+    auto pack_columns = [&](const void* src, int64_t n, uint16_t* to, uint32_t half, const float* dl, const float* tops, float* top) {
         const dim3 grid((unsigned)((half / (p.f32 ? 2 : 1) + 63) / 64), columns);
-        if (p.f32) pack_columns_kernel<float><<<grid, 256, 0, st>>>((const float*)src, n, width, to, half, dl, top);
-        else pack_columns_kernel<uint16_t><<<grid, 256, 0, st>>>((const uint16_t*)src, n, width, to, half, dl, top);
+        if (p.f32) columns_kernel<float><<<grid, 256, 0, st>>>((const float*)src, n, width, to, half, dl, tops, rows_grid(n), top);
+        else columns_kernel<uint16_t><<<grid, 256, 0, st>>>((const uint16_t*)src, n, width, to, half, dl, tops, rows_grid(n), top);
+        return launched();
     };
-    if (dx) pack_columns(w, vocab, a.wt, a.wt_half, nullptr, a.tops + 2);
-    if (dw) pack_columns(x, rows, a.xt, a.xt_half, a.dl, a.tops + 1);
-    if (int rc = launched()) return rc;
+    int rc = 0;
+    if (dx && (rc = pack_columns(w, vocab, a.wt, a.wt_half, nullptr, a.tops + kTops, a.top + 2))) return rc;
+    if (dw && (rc = pack_columns(x, rows, a.xt, a.xt_half, a.dl, a.tops, a.top + 1))) return rc;
     Logits l = logits_of(p, a.sides, x, w, target);
     const int tile = p.tile(), per = p.per_step();
     for (int v0 = 0; v0 < vocab; v0 += a.piece) {
-        const int entries = vocab - v0 < a.piece ? vocab - v0 : a.piece;
+        const int entries = a.entries_of(p, v0);
+        const bool last = v0 + a.piece >= vocab;
         l.v0 = v0;
         l.tiles_v = (entries + p.bv() - 1) / p.bv();
         uint16_t *g = dx ? a.g : nullptr, *gt = dw ? a.gt : nullptr;
-        int rc;
         if (p.f32) rc = tile == 0 ? run_grad<Big2>(l, lse, a, g, gt, st) : tile == 1 ? run_grad<Mid2>(l, lse, a, g, gt, st) : run_grad<Low2>(l, lse, a, g, gt, st);
         else rc = tile == 0 ? run_grad<Big>(l, lse, a, g, gt, st) : tile == 1 ? run_grad<Mid>(l, lse, a, g, gt, st) : run_grad<Low>(l, lse, a, g, gt, st);
         if (rc) return rc;
         if (dx) {
             // features inside, rows of x outside
-            const NtOperand A{a.wt + (size_t)v0 / per * 64, width, a.wt_half * 2}, B{a.g, rows, a.g_half * 2};
-            const int steps = (entries + per - 1) / per;
-            const bool first = v0 == 0, last = v0 + a.piece >= vocab;
-            if (p.f32) rc = product<Big2, Mid2, float>(A, B, steps, (float*)dx, width, (float*)dx, !first, false, a.tops + 2, a.tops, st);
-            else rc = product<Big, Mid, uint16_t>(A, B, steps, (uint16_t*)dx, width, a.sum, !first, !last, nullptr, nullptr, st);
+            Job j{{a.wt + (size_t)v0 / per * 64, width, a.wt_half * 2}, {a.g, rows, a.g_half * 2}, (entries + per - 1) / per, dx, width, a.dx_part, v0 > 0,
+                  last, {a.top + 2, nullptr, a.dl}};
+            rc = p.f32 ? product<Big2, Mid2, float>(j, a.dx_cut, st) : product<Big16, Mid16, uint16_t>(j, a.dx_cut, st);
             if (rc) return rc;
         }
         if (dw) {
-            const NtOperand A{a.xt, width, a.xt_half * 2}, B{a.gt, entries, a.gt_half * 2};
-            const int steps = (int)((rows + per - 1) / per);
+            const Cut& cut = last ? a.dw_last : a.dw_cut;
+            Job j{{a.xt, width, a.xt_half * 2}, {a.gt, entries, a.gt_half * 2}, (int)((rows + per - 1) / per), nullptr, width,
+                  cut.shares > 1 ? a.dw_part : nullptr, false, true, {a.top + 1, a.top, nullptr}};
             const size_t at = (size_t)v0 * width;
-            if (p.f32) rc = product<Big2, Mid2, float>(A, B, steps, (float*)dw + at, width, nullptr, false, false, a.tops + 1, a.tops, st);
-            else if (dw_f32) rc = product<Big, Mid, float>(A, B, steps, (float*)dw + at, width, nullptr, false, false, nullptr, nullptr, st);
-            else rc = product<Big, Mid, uint16_t>(A, B, steps, (uint16_t*)dw + at, width, nullptr, false, false, nullptr, nullptr, st);
+            if (dw_f32) {
+                j.out = (float*)dw + at;
+                rc = p.f32 ? product<Big2, Mid2, float>(j, cut, st) : product<Big16, Mid16, float>(j, cut, st);
+            } else {
+                j.out = (uint16_t*)dw + at;
+                rc = product<Big16, Mid16, uint16_t>(j, cut, st);
+            }
             if (rc) return rc;
         }
     }

@@ -1,10 +1,14 @@
 // Products of two row-major operands along their rows, D[m][n] = sum_k A[m][k] B[n][k], as a tile of a workgroup: the core of the
 // loss over a vocabulary and of the orthogonalised updates.
 //
-// An operand is rows of 128-byte steps of 16-bit numbers.  One plane (PL = 1): a step is 64 numbers along k.  Two planes (PL = 2): a
-// step is 32 numbers along k, the upper parts first, then what they leave; the product takes upper x upper and the two mixed ones, and
-// leaves out lower x lower (2^-22 of the product for binary16 planes).
+// An operand is rows of 128-byte steps.  What a step holds goes by the kind:
+//   kBf16, kF16     64 numbers along k
+//   kF16x2          32 numbers along k in two binary16 planes, the upper parts first, then what they leave; the product takes upper x
+//                   upper and the two mixed ones, and leaves out lower x lower (2^-22 of the product)
+//   kF32            32 fp32 numbers along k, on the fp32 matrix instruction (a sixteenth of the bf16 rate)
 #pragma once
+#include <type_traits>
+
 #include "monarch_mfma_common.h"
 
 namespace monarch {
@@ -17,26 +21,47 @@ struct NtOperand {
     uint32_t row_bytes;  // a multiple of 16; a tile's rows stay below 2^31 bytes
 };
 
+enum NtKind { kBf16, kF16, kF16x2, kF32 };
+
 // A workgroup's BM x BN tile, a wave's WM x WN part of it.
-template <int BM_, int BN_, int WM_, int WN_, int PL_, bool F16_>
+template <int BM_, int BN_, int WM_, int WN_, NtKind KIND_, int RING_ = 2>
 struct NtTile {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, PL = PL_;
-    static constexpr bool F16 = F16_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, RING = RING_;  // RING: steps in LDS
+    static constexpr NtKind KIND = KIND_;
+    static constexpr int PL = KIND == kF16x2 ? 2 : 1;  // planes
     static constexpr int WAVES = (BM / WM) * (BN / WN), THREADS = 64 * WAVES;
     static constexpr int TI = WM / 16, TJ = WN / 16;
-    static constexpr int BUFFER = (BM + BN) * 128, LDS_BYTES = 2 * BUFFER;
+    static constexpr int BUFFER = (BM + BN) * 128, LDS_BYTES = RING * BUFFER;
     static constexpr int ASK_A = BM / 8 / WAVES, ASK_B = BN / 8 / WAVES;  // requests of a wave per step, 8 rows each
+    static_assert(RING >= 2 && RING <= 4, "ring");
     static_assert(ASK_A * 8 * WAVES == BM && ASK_B * 8 * WAVES == BN, "whole requests");
     static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
     static __device__ __forceinline__ int row0() { return wave() / (BN / WN) * WM; }  // of the wave's part
     static __device__ __forceinline__ int col0() { return wave() % (BN / WN) * WN; }
 };
 
-template <bool F16>
-__device__ __forceinline__ f32x4 nt_mfma(u32x4 a, u32x4 b, f32x4 c)
+__device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// c += what a step's two halves of the operands contribute
+template <NtKind KIND>
+__device__ __forceinline__ f32x4 nt_step(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1, f32x4 c)
 {
-    if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    else return mfma16(as_bf16x8(a), as_bf16x8(b), c);
+    if constexpr (KIND == kBf16) {
+        c = mfma16(as_bf16x8(a0), as_bf16x8(b0), c);
+        return mfma16(as_bf16x8(a1), as_bf16x8(b1), c);
+    } else if constexpr (KIND == kF32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a0[e]), __uint_as_float(b0[e]), c, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a1[e]), __uint_as_float(b1[e]), c, 0, 0, 0);
+        return c;
+    } else {
+        const f16x8 p0 = __builtin_bit_cast(f16x8, a0), p1 = __builtin_bit_cast(f16x8, a1), q0 = __builtin_bit_cast(f16x8, b0), q1 = __builtin_bit_cast(f16x8, b1);
+        c = mfma16(p0, q0, c);
+        if constexpr (KIND == kF16) return mfma16(p1, q1, c);
+        c = mfma16(p0, q1, c);
+        return mfma16(p1, q0, c);
+    }
 }
 
 #ifdef __HIP_DEVICE_COMPILE__
@@ -50,11 +75,12 @@ __device__ __forceinline__ auto nt_rsrc(const NtOperand& o, int64_t row, int row
 #endif
 
 // acc[i][j][e] = D[a0 + row0() + 16 i + 4 (lane / 16) + e][b0 + col0() + 16 j + lane % 16] over `steps` steps from `step0`.
-// Double buffer: while a step's products run, the next one's 128-byte rows come straight into the other half of LDS.  16-byte piece u
-// of row r lies in place u ^ (r % 8), so that the 16 rows of a fragment fall on different banks.
-template <typename C>
+// The 128-byte rows of the next RING - 1 steps come straight into LDS while a step's products run; one barrier a step.  16-byte piece u
+// of row r lies in place u ^ (r % 8), so that the 16 rows of a fragment fall on different banks.  TAIL: only the first `tail` of the eight
+// pieces of the last step count (the rows end there, and what follows is not theirs).
+template <typename C, bool TAIL = false>
 __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const NtOperand& B, int64_t b0, int step0, int steps,
-                                           unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ])
+                                           unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int tail = 8)
 {
 #pragma unroll
     for (int i = 0; i < C::TI; ++i)
@@ -83,34 +109,42 @@ __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const
     const int r16 = lane & 15, at0 = 16 * ((lane >> 4) ^ (lane & 7)), at1 = at0 ^ 64;
     const unsigned char* fa = lds + (C::row0() + r16) * 128;
     const unsigned char* fb = lds + C::BM * 128 + (C::col0() + r16) * 128;
-    if (steps > 0) ask(step0, 0);
-    for (int s = 0; s < steps; ++s) {
-        const int buffer = s & 1;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (s + 1 < steps) ask(step0 + s + 1, buffer ^ 1);
-        const unsigned char *pa = fa + buffer * C::BUFFER, *pb = fb + buffer * C::BUFFER;
+    auto products = [&](auto cut, const unsigned char* pa, const unsigned char* pb) {
+        const bool in0 = lane >> 4 < tail, in1 = 4 + (lane >> 4) < tail;
+        auto half = [&](const unsigned char* p, bool in) {
+            u32x4 v = lds128(p);
+            if constexpr (decltype(cut)::value)
+                if (!in) v = u32x4{0, 0, 0, 0};
+            return v;
+        };
         u32x4 b[2][C::TJ];
 #pragma unroll
         for (int j = 0; j < C::TJ; ++j) {
-            b[0][j] = lds128(pb + j * 2048 + at0);
-            b[1][j] = lds128(pb + j * 2048 + at1);
+            b[0][j] = half(pb + j * 2048 + at0, in0);
+            b[1][j] = half(pb + j * 2048 + at1, in1);
         }
 #pragma unroll
         for (int i = 0; i < C::TI; ++i) {
-            const u32x4 a0 = lds128(pa + i * 2048 + at0), a1 = lds128(pa + i * 2048 + at1);
+            const u32x4 a0 = half(pa + i * 2048 + at0, in0), a1 = half(pa + i * 2048 + at1, in1);
 #pragma unroll
-            for (int j = 0; j < C::TJ; ++j) {
-                acc[i][j] = nt_mfma<C::F16>(a0, b[0][j], acc[i][j]);
-                if constexpr (C::PL == 1) {
-                    acc[i][j] = nt_mfma<C::F16>(a1, b[1][j], acc[i][j]);
-                } else {
-                    acc[i][j] = nt_mfma<C::F16>(a0, b[1][j], acc[i][j]);
-                    acc[i][j] = nt_mfma<C::F16>(a1, b[0][j], acc[i][j]);
-                }
-            }
+            for (int j = 0; j < C::TJ; ++j) acc[i][j] = nt_step<C::KIND>(a0, a1, b[0][j], b[1][j], acc[i][j]);
         }
+    };
+    constexpr int ASKS = C::ASK_A + C::ASK_B;
+    for (int s = 0; s < C::RING - 1 && s < steps; ++s) ask(step0 + s, s);
+    int buffer = 0;
+    for (int s = 0; s < steps; ++s) {
+        // step s has landed once only what was asked for after it is outstanding
+        if (C::RING == 4 && s + 2 < steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * ASKS) : "memory");
+        else if (C::RING >= 3 && s + 1 < steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(ASKS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();  // ... for every wave, and nobody reads step s - 1 any more
+        asm volatile("" ::: "memory");
+        if (s + C::RING - 1 < steps) ask(step0 + s + C::RING - 1, buffer ? buffer - 1 : C::RING - 1);
+        const unsigned char *pa = fa + buffer * C::BUFFER, *pb = fb + buffer * C::BUFFER;
+        if (TAIL && s + 1 == steps && tail < 8) products(std::true_type{}, pa, pb);
+        else products(std::false_type{}, pa, pb);
+        buffer = buffer + 1 == C::RING ? 0 : buffer + 1;
     }
 #endif
 }

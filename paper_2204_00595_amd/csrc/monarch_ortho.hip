@@ -300,8 +300,8 @@ int run_product(Product p, const Sink& sink, hipStream_t st)
 template <Part PART, typename T, Out OUT>
 int product(const Product& p, const Sink& sink, hipStream_t st)
 {
-    using Low = NtTile<64, 64, 32, 32, 2, true>;
-    using Mid = NtTile<128, 128, 64, 64, 2, true>;
+    using Low = NtTile<64, 64, 32, 32, kF16x2, 4>;
+    using Mid = NtTile<128, 128, 64, 64, kF16x2>;
     const int64_t mid = (int64_t)((p.a_rows + 127) / 128) * ((p.b_rows + 127) / 128) * p.blocks;
     return mid >= 256 ? run_product<Mid, PART, T, OUT>(p, sink, st) : run_product<Low, PART, T, OUT>(p, sink, st);
 }

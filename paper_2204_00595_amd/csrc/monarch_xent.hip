@@ -55,6 +55,22 @@ __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 
 // ---- operands ----
 
+// eight numbers times `up` as binary16 in their places: one plane, or two
+template <bool PLANES>
+__device__ __forceinline__ void store_planes(uint16_t* at, const float (&v)[8], float up)
+{
+    uint32_t hi[8], lo[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        uint16_t h, l;
+        split2(v[e] * up, h, l);
+        hi[e] = h;
+        lo[e] = l;
+    }
+    *reinterpret_cast<u32x4*>(at) = u32x4{hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16};
+    if constexpr (PLANES) *reinterpret_cast<u32x4*>(at + 32) = u32x4{lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16};
+}
+
 constexpr int kTops = 1024;  // workgroups, at most, that leave the largest magnitude they met
 
 // Largest finite magnitude of `n` values (a workgroup of 256).
@@ -94,7 +110,14 @@ __global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, in
                 m = fmaxf(m, __uint_as_float(t << 16));
             }
         } else {
-            for (int k = lane; k < width; k += 64) m = fmaxf(m, finite_magnitude(Elem<T>::load(s + k)));
+            const int quads = sizeof(T) == 4 && (width & 3) == 0 ? width / 4 : 0;
+            if constexpr (sizeof(T) == 4)
+                for (int k = lane; k < quads; k += 64) {
+                    const f32x4 u = *reinterpret_cast<const f32x4*>(s + 4 * k);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_magnitude(u[e]));
+                }
+            for (int k = 4 * quads + lane; k < width; k += 64) m = fmaxf(m, finite_magnitude(Elem<T>::load(s + k)));
         }
         m = wave_all(m, max_of);
         if (!(dl && dl[row] == 0.f)) all = fmaxf(all, m);
@@ -105,12 +128,19 @@ __global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, in
         } else {
             const float up = scale_for(m);
             if (lane == 0) inv[row] = inverse_power(up);
-            for (uint32_t k = lane; k < row_half / 2; k += 64) {
-                uint16_t hi = 0, lo = 0;
-                if (k < (uint32_t)width) split2(s[k] * up, hi, lo);
-                uint16_t* at = d + (k >> 5) * 64 + (k & 31);
-                at[0] = hi;
-                at[32] = lo;
+            for (uint32_t k = lane * 8; k < row_half / 2; k += 512) {
+                float v[8];
+                if ((width & 3) == 0) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 4) {
+                        const f32x4 u = k + e < (uint32_t)width ? *reinterpret_cast<const f32x4*>(s + k + e) : f32x4{0.f, 0.f, 0.f, 0.f};
+                        v[e] = u[0], v[e + 1] = u[1], v[e + 2] = u[2], v[e + 3] = u[3];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = k + e < (uint32_t)width ? s[k + e] : 0.f;
+                }
+                store_planes<true>(d + (k >> 5) * 64 + (k & 31), v, up);
             }
         }
     }
@@ -159,18 +189,10 @@ __global__ __launch_bounds__(256) void columns_kernel(const T* __restrict__ src,
         const int piece = i * 256 + tid, c = piece >> 3, r = (piece & 7) * 8;
         const int64_t k = k0 + r;
         if (c0 + c >= width || k * (kPlanes ? 2 : 1) >= (int64_t)row_half) continue;
-        uint32_t hi[8], lo[8];
+        float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            uint16_t h, l;
-            split2(tile[r + e][c] * up, h, l);
-            hi[e] = h;
-            lo[e] = l;
-        }
-        uint16_t* at = dst + (int64_t)(c0 + c) * row_half + (kPlanes ? (k >> 5) * 64 + (k & 31) : k);
-        *reinterpret_cast<u32x4*>(at) = u32x4{hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16};
-        if constexpr (kPlanes)
-            *reinterpret_cast<u32x4*>(at + 32) = u32x4{lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16};
+        for (int e = 0; e < 8; ++e) v[e] = tile[r + e][c];
+        store_planes<kPlanes>(dst + (int64_t)(c0 + c) * row_half + (kPlanes ? (k >> 5) * 64 + (k & 31) : k), v, up);
     }
 }
 
@@ -181,14 +203,14 @@ struct Logits {
     const float *winv, *xinv;  // two planes: inverse powers of two of their rows
     const int64_t* target;
     int64_t rows;
-    int vocab, steps;
+    int vocab, steps, tail;
     int v0, tiles_v, tiles_t;  // the piece of the vocabulary: entries v0 .. of it
 };
 
-template <typename C>
+template <typename C, bool TAIL>
 __device__ __forceinline__ void logits_tile(const Logits& p, int64_t v0, int64_t t0, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ])
 {
-    nt_product<C>(p.w, v0, p.x, t0, 0, p.steps, lds, acc);
+    nt_product<C, TAIL>(p.w, v0, p.x, t0, 0, p.steps, lds, acc, p.tail);
     if constexpr (C::PL == 2) {
         const int lane = threadIdx.x & 63;
         float xi[C::TJ];
@@ -209,8 +231,23 @@ __device__ __forceinline__ void logits_tile(const Logits& p, int64_t v0, int64_t
     }
 }
 
-// Largest (in units of log 2) and sum of the tile's entries for each of its rows of x -> part[t][tile]; the target's logit -> hit[t].
+// Where the target of row t lies among the tile's entries (negative or BM and more: elsewhere).
 template <typename C>
+__device__ __forceinline__ int target_at(const Logits& p, int64_t t, int64_t v0)
+{
+    const int64_t at = t < p.rows ? p.target[t] - v0 : -1;
+    return at < 0 || at >= C::BM || v0 + at >= p.vocab ? -C::BM : (int)at;
+}
+
+// Largest (in units of log 2) and sum of two parts as one
+__device__ __forceinline__ f32x2 joined(f32x2 a, f32x2 b)
+{
+    const float m = fmaxf(a[0], b[0]), base = m == -__builtin_inff() ? 0.f : m;
+    return f32x2{m, a[1] * exp2_fast(a[0] - base) + b[1] * exp2_fast(b[0] - base)};
+}
+
+// Largest (in units of log 2) and sum of the tile's entries for each of its rows of x -> part[t][tile]; the target's logit -> hit[t].
+template <typename C, bool TAIL>
 __global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* __restrict__ part, int parts, float* __restrict__ hit)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
@@ -218,25 +255,39 @@ __global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* 
     if (!nt_place(blockIdx.x, p.tiles_v, p.tiles_t, tv, tt)) return;
     const int64_t v0 = (int64_t)tv * C::BM, t0 = (int64_t)tt * C::BN;
     f32x4 acc[C::TI][C::TJ];
-    logits_tile<C>(p, v0, t0, lds, acc);
+    logits_tile<C, TAIL>(p, v0, t0, lds, acc);
     const int lane = threadIdx.x & 63;
     const int vr = C::row0() + 4 * (lane >> 4);
-    const int64_t left = p.vocab - v0 - vr;  // entries from the lane's first on
     f32x2* red = reinterpret_cast<f32x2*>(lds);  // [BM / WM][BN]
+    if (v0 + C::BM > p.vocab) {
+        const int left = (int)(p.vocab - v0) - vr;  // entries from the lane's first on
+#pragma unroll
+        for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (16 * i + e >= left)
+#pragma unroll
+                    for (int j = 0; j < C::TJ; ++j) acc[i][j][e] = -__builtin_inff();
+    }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j) {
         const int64_t t = t0 + C::col0() + 16 * j + (lane & 15);
-        const int64_t at = t < p.rows ? p.target[t] - v0 - vr : -1;  // the target among the lane's entries
+        const int at = target_at<C>(p, t, v0) - vr;  // the target among the lane's entries
+        const bool mine = at >= 0 && at < C::WM && (at & 15) < 4;
+        if (__any(mine)) {  // (one tile of the vocabulary holds a row's target)
+            float l = 0.f;
+#pragma unroll
+            for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) l = at == 16 * i + e ? acc[i][j][e] : l;
+            if (mine) hit[t] = l;
+        }
         float m = -__builtin_inff();
 #pragma unroll
         for (int i = 0; i < C::TI; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (at == 16 * i + e) hit[t] = acc[i][j][e];
-                if (16 * i + e >= left) acc[i][j][e] = -__builtin_inff();
-                m = fmaxf(m, acc[i][j][e]);
-            }
+            for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
         m *= kLog2e;
@@ -256,11 +307,7 @@ __global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* 
         if (t >= p.rows) break;
         f32x2 r = red[c];
 #pragma unroll
-        for (int k = 1; k < C::BM / C::WM; ++k) {
-            const f32x2 o = red[k * C::BN + c];
-            const float m = fmaxf(r[0], o[0]), b = m == -__builtin_inff() ? 0.f : m;
-            r = f32x2{m, r[1] * exp2_fast(r[0] - b) + o[1] * exp2_fast(o[0] - b)};
-        }
+        for (int k = 1; k < C::BM / C::WM; ++k) r = joined(r, red[k * C::BN + c]);
         part[t * parts + tv] = r;
     }
 }
@@ -322,7 +369,7 @@ constexpr float kG = 0x1p14f;  // what exp(l - lse) - [v = target] is stored tim
 // G of a piece of the vocabulary as operands of binary16 planes: once with the vocabulary last and without the upstream gradient, which dx
 // takes row by row (g), and once with the rows of x last and with it, times the power of two for the largest one (gt).  Both leave by
 // way of LDS in runs of 64 bytes and more.  Entries and rows that do not exist are written as zeros.
-template <typename C>
+template <typename C, bool TAIL>
 __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const float* __restrict__ lse, const float* __restrict__ dl,
                                                                const float* __restrict__ dl_top, uint16_t* __restrict__ g, uint32_t g_half,
                                                                uint16_t* __restrict__ gt, uint32_t gt_half)
@@ -332,10 +379,10 @@ __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const f
     if (!nt_place(blockIdx.x, p.tiles_v, p.tiles_t, tv, tt)) return;
     const int64_t v0 = p.v0 + (int64_t)tv * C::BM, t0 = (int64_t)tt * C::BN;
     f32x4 acc[C::TI][C::TJ];
-    logits_tile<C>(p, v0, t0, lds, acc);
+    logits_tile<C, TAIL>(p, v0, t0, lds, acc);
     const int tid = threadIdx.x, lane = tid & 63;
     const int vr = C::row0() + 4 * (lane >> 4), tc = C::col0() + (lane & 15);
-    const int64_t left = p.vocab - v0 - vr;
+    const int left = p.vocab - v0 - vr < C::BM ? (int)(p.vocab - v0) - vr : C::BM;
     const float up = scale_for(*dl_top);
     float d[C::TJ];
 #pragma unroll
@@ -344,15 +391,23 @@ __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const f
         const bool row = t < p.rows;
         const float ls = row ? lse[t] : 0.f;
         d[j] = row ? dl[t] * up : 0.f;
-        const int64_t at = row ? p.target[t] - v0 - vr : -1;
 #pragma unroll
         for (int i = 0; i < C::TI; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float s = exp2_fast((acc[i][j][e] - ls) * kLog2e);
-                if (at == 16 * i + e) s -= 1.f;
-                acc[i][j][e] = d[j] == 0.f || 16 * i + e >= left ? 0.f : s;
-            }
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = exp2_fast((acc[i][j][e] - ls) * kLog2e);
+        const int at = target_at<C>(p, t, v0) - vr;
+        if (__any(at >= 0 && at < C::WM)) {
+#pragma unroll
+            for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = at == 16 * i + e ? acc[i][j][e] - 1.f : acc[i][j][e];
+        }
+        if (__any(d[j] == 0.f) || left < C::WM) {  // rows that do not count, entries that do not exist
+#pragma unroll
+            for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = d[j] == 0.f || 16 * i + e >= left ? 0.f : acc[i][j][e];
+        }
     }
     // plane `plane` of four numbers times `by`
     auto four = [&](const f32x4& s, float by, int plane) {
@@ -512,14 +567,18 @@ __global__ __launch_bounds__(1024) void xent_total_kernel(const float* __restric
 
 // ---- plans ----
 
-using Big = NtTile<256, 256, 128, 64, 1, false>;
-using Mid = NtTile<128, 128, 64, 64, 1, false>;
-using Low = NtTile<128, 64, 32, 64, 1, false>;
-using Big2 = NtTile<256, 256, 128, 64, 2, true>;
-using Mid2 = NtTile<128, 128, 64, 64, 2, true>;
-using Low2 = NtTile<128, 64, 32, 64, 2, true>;
-using Big16 = NtTile<256, 256, 128, 64, 1, true>;
-using Mid16 = NtTile<128, 128, 64, 64, 1, true>;
+using Big = NtTile<256, 256, 128, 64, kBf16>;
+using Mid = NtTile<128, 128, 64, 64, kBf16>;
+using Low = NtTile<128, 64, 32, 64, kBf16>;
+using FewB = NtTile<128, 32, 32, 32, kBf16, 4>;
+using Big2 = NtTile<256, 256, 128, 64, kF16x2>;
+using Mid2 = NtTile<128, 128, 64, 64, kF16x2>;
+using Low2 = NtTile<128, 64, 32, 64, kF16x2>;
+using Few2 = NtTile<128, 32, 32, 32, kF16x2>;
+using Low32 = NtTile<128, 64, 32, 64, kF32, 3>;
+using Few32 = NtTile<128, 32, 32, 32, kF32, 4>;
+using Big16 = NtTile<256, 256, 128, 64, kF16>;
+using Mid16 = NtTile<128, 128, 64, 64, kF16>;
 
 // bytes handed out of a workspace
 struct Area {
@@ -540,15 +599,29 @@ struct Plan {
     int vocab, width;
     int per_step() const { return f32 ? 32 : 64; }  // numbers along k in a step
     uint32_t half(int64_t k) const { return (uint32_t)((k + per_step() - 1) / per_step() * 64); }  // 16-bit numbers of an operand's row
-    // bf16 rows that are whole steps serve as they are
-    bool packs() const { return f32 || width % 64 != 0; }
-    // tile of the logits: 0 = 256 x 256, 1 = 128 x 128, 2 = 128 entries x 64 rows
-    int tile() const { return rows > 128 ? 0 : rows > 64 ? 1 : 2; }
+    bool forward;  // else the gradients
+    // Up to 64 rows the forward of fp32 tensors is bound by reading W, and the fp32 matrix instruction keeps up with that.
+    bool plain32() const { return f32 && forward && rows <= 64 && width % 4 == 0; }
+    // rows of whole 16-byte pieces serve as they are
+    bool packs() const { return f32 ? !plain32() : width % 8 != 0; }
+    // tile of the logits: 0 = 256 x 256, 1 = 128 x 128, 2 = 128 entries x 64 rows, 3 = 128 x 32 (forward)
+    int tile() const { return rows > 128 ? 0 : rows > 64 ? 1 : rows > 32 || !forward ? 2 : 3; }
     int bv() const { return tile() == 0 ? 256 : 128; }
-    int bt() const { return tile() == 0 ? 256 : tile() == 1 ? 128 : 64; }
+    int bt() const { return tile() == 0 ? 256 : tile() == 1 ? 128 : tile() == 2 ? 64 : 32; }
     int parts() const { return (vocab + bv() - 1) / bv(); }
     int64_t row_tiles() const { return (rows + bt() - 1) / bt(); }
 };
+
+template <typename A, typename B, typename C, typename D, typename F>
+int by_tile(const Plan& p, F f)
+{
+    switch (p.tile()) {
+        case 0: return f(A{});
+        case 1: return f(B{});
+        case 2: return f(C{});
+        default: return f(D{});
+    }
+}
 
 struct Sides {  // x and W as operands, with their powers of two
     uint16_t *x = nullptr, *w = nullptr;
@@ -682,7 +755,7 @@ int pack_sides(const Plan& p, const Sides& s, const void* x, const void* w, cons
 
 Logits logits_of(const Plan& p, const Sides& s, const void* x, const void* w, const int64_t* target)
 {
-    const uint32_t bytes = p.half(p.width) * 2;
+    const uint32_t bytes = p.packs() ? p.half(p.width) * 2 : (uint32_t)p.width * (p.f32 ? 4 : 2);
     Logits l;
     l.w = NtOperand{p.packs() ? s.w : w, p.vocab, bytes};
     l.x = NtOperand{p.packs() ? s.x : x, p.rows, bytes};
@@ -691,25 +764,32 @@ Logits logits_of(const Plan& p, const Sides& s, const void* x, const void* w, co
     l.target = target;
     l.rows = p.rows;
     l.vocab = p.vocab;
-    l.steps = (int)(bytes / 128);
+    l.steps = (int)((bytes + 127) / 128);
+    l.tail = (int)(bytes % 128 / 16);
+    if (!l.tail) l.tail = 8;
     l.v0 = 0;
     l.tiles_v = p.parts();
     l.tiles_t = (int)p.row_tiles();
     return l;
 }
 
-template <typename C>
+// Rows that end inside a step have kernels of their own (the test for it in every step costs 14 % of a long product).
+template <typename C, bool TAIL>
 int run_part(const Logits& l, f32x2* part, int parts, float* hit, hipStream_t st)
 {
-    if (allow_dynamic_lds((const void*)xent_part_kernel<C>, C::LDS_BYTES) != hipSuccess) return -4;
-    xent_part_kernel<C><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, part, parts, hit);
+    if constexpr (!TAIL && C::KIND != kF16x2)
+        if (l.tail < 8) return run_part<C, true>(l, part, parts, hit, st);
+    if (allow_dynamic_lds((const void*)xent_part_kernel<C, TAIL>, C::LDS_BYTES) != hipSuccess) return -4;
+    xent_part_kernel<C, TAIL><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, part, parts, hit);
     return launched();
 }
-template <typename C>
+template <typename C, bool TAIL>
 int run_grad(const Logits& l, const float* lse, const BwdArea& a, uint16_t* g, uint16_t* gt, hipStream_t st)
 {
-    if (allow_dynamic_lds((const void*)xent_grad_kernel<C>, C::LDS_BYTES) != hipSuccess) return -4;
-    xent_grad_kernel<C><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, lse, a.dl, a.top, g, a.g_half, gt, a.gt_half);
+    if constexpr (!TAIL && C::KIND != kF16x2)
+        if (l.tail < 8) return run_grad<C, true>(l, lse, a, g, gt, st);
+    if (allow_dynamic_lds((const void*)xent_grad_kernel<C, TAIL>, C::LDS_BYTES) != hipSuccess) return -4;
+    xent_grad_kernel<C, TAIL><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, lse, a.dl, a.top, g, a.g_half, gt, a.gt_half);
     return launched();
 }
 
@@ -751,31 +831,32 @@ bool xent_supported(int64_t rows, int vocab, int width)
 size_t xent_fwd_workspace(int64_t rows, int vocab, int width, int dtype)
 {
     FwdArea a;
-    return rows ? a.lay(Plan{dtype == 0, rows, vocab, width}, nullptr) : 0;
+    return rows ? a.lay(Plan{dtype == 0, rows, vocab, width, true}, nullptr) : 0;
 }
 size_t xent_bwd_workspace(int64_t rows, int vocab, int width, int dtype)
 {
     BwdArea a;
-    return rows ? a.fit(Plan{dtype == 0, rows, vocab, width}, nullptr, (size_t)-1) : 0;
+    return rows ? a.fit(Plan{dtype == 0, rows, vocab, width, false}, nullptr, (size_t)-1) : 0;
 }
 size_t xent_bwd_least(int64_t rows, int vocab, int width, int dtype)
 {
     BwdArea a;
-    return rows ? a.lay(Plan{dtype == 0, rows, vocab, width}, nullptr, 1) : 0;
+    return rows ? a.lay(Plan{dtype == 0, rows, vocab, width, false}, nullptr, 1) : 0;
 }
 
 int xent_fwd(const void* x, const void* w, const int64_t* target, float* loss, float* lse, int64_t rows, int vocab, int width, int64_t ignore,
              int dtype, void* ws, hipStream_t st)
 {
-    const Plan p{dtype == 0, rows, vocab, width};
+    const Plan p{dtype == 0, rows, vocab, width, true};
     FwdArea a;
     a.lay(p, (char*)ws);
     if (int rc = pack_sides(p, a.sides, x, w, nullptr, nullptr, st)) return rc;
     const Logits l = logits_of(p, a.sides, x, w, target);
-    const int parts = p.parts(), tile = p.tile();
+    const int parts = p.parts();
     int rc;
-    if (p.f32) rc = tile == 0 ? run_part<Big2>(l, a.part, parts, a.hit, st) : tile == 1 ? run_part<Mid2>(l, a.part, parts, a.hit, st) : run_part<Low2>(l, a.part, parts, a.hit, st);
-    else rc = tile == 0 ? run_part<Big>(l, a.part, parts, a.hit, st) : tile == 1 ? run_part<Mid>(l, a.part, parts, a.hit, st) : run_part<Low>(l, a.part, parts, a.hit, st);
+    if (p.plain32()) rc = p.rows > 32 ? run_part<Low32, false>(l, a.part, parts, a.hit, st) : run_part<Few32, false>(l, a.part, parts, a.hit, st);
+    else if (p.f32) rc = by_tile<Big2, Mid2, Low2, Few2>(p, [&](auto c) { return run_part<decltype(c), false>(l, a.part, parts, a.hit, st); });
+    else rc = by_tile<Big, Mid, Low, FewB>(p, [&](auto c) { return run_part<decltype(c), false>(l, a.part, parts, a.hit, st); });
     if (rc) return rc;
     xent_join_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a.part, parts, a.hit, target, ignore, vocab, rows, loss, lse);
     return launched();
@@ -784,7 +865,7 @@ int xent_fwd(const void* x, const void* w, const int64_t* target, float* loss, f
 int xent_bwd(const void* x, const void* w, const int64_t* target, const float* lse, const float* dloss, int64_t dloss_stride, const float* divisor,
              void* dx, void* dw, int64_t rows, int vocab, int width, int64_t ignore, int dtype, bool dw_f32, void* ws, size_t ws_bytes, hipStream_t st)
 {
-    const Plan p{dtype == 0, rows, vocab, width};
+    const Plan p{dtype == 0, rows, vocab, width, false};
     BwdArea a;
     if (!a.fit(p, (char*)ws, ws_bytes)) return -3;
     xent_upstream_kernel<<<1, 1024, 0, st>>>(dloss, dloss_stride, divisor, target, ignore, vocab, rows, a.dl, a.top);
@@ -801,15 +882,15 @@ int xent_bwd(const void* x, const void* w, const int64_t* target, const float* l
     if (dx && (rc = pack_columns(w, vocab, a.wt, a.wt_half, nullptr, a.tops + kTops, a.top + 2))) return rc;
     if (dw && (rc = pack_columns(x, rows, a.xt, a.xt_half, a.dl, a.tops, a.top + 1))) return rc;
     Logits l = logits_of(p, a.sides, x, w, target);
-    const int tile = p.tile(), per = p.per_step();
+    const int per = p.per_step();
     for (int v0 = 0; v0 < vocab; v0 += a.piece) {
         const int entries = a.entries_of(p, v0);
         const bool last = v0 + a.piece >= vocab;
         l.v0 = v0;
         l.tiles_v = (entries + p.bv() - 1) / p.bv();
         uint16_t *g = dx ? a.g : nullptr, *gt = dw ? a.gt : nullptr;
-        if (p.f32) rc = tile == 0 ? run_grad<Big2>(l, lse, a, g, gt, st) : tile == 1 ? run_grad<Mid2>(l, lse, a, g, gt, st) : run_grad<Low2>(l, lse, a, g, gt, st);
-        else rc = tile == 0 ? run_grad<Big>(l, lse, a, g, gt, st) : tile == 1 ? run_grad<Mid>(l, lse, a, g, gt, st) : run_grad<Low>(l, lse, a, g, gt, st);
+        if (p.f32) rc = by_tile<Big2, Mid2, Low2, Low2>(p, [&](auto c) { return run_grad<decltype(c), false>(l, lse, a, g, gt, st); });
+        else rc = by_tile<Big, Mid, Low, Low>(p, [&](auto c) { return run_grad<decltype(c), false>(l, lse, a, g, gt, st); });
         if (rc) return rc;
         if (dx) {
             // features inside, rows of x outside

@@ -183,6 +183,14 @@ struct Sink {  // kLast: out[b][a], rows of n
 };
 enum Out { kPlain, kWeights, kMasters };  // x itself; weights updated; fp32 masters updated, weights their rounding
 
+template <typename T, Out OUT>
+__device__ __forceinline__ void put(const Sink& sink, T* out, float* master, float x)
+{
+    if constexpr (OUT == kWeights) x = fmaf(-sink.rate, x, sink.keep * Elem<T>::load(out));
+    if constexpr (OUT == kMasters) *master = x = fmaf(-sink.rate, x, sink.keep * *master);
+    Elem<T>::store(out, x);
+}
+
 template <typename C, Part PART, typename T, Out OUT>
 __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Sink sink)
 {
@@ -212,10 +220,7 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (m + e >= p.a_rows) break;
-                    float x = v[e] * (1.f / (kX * kP));
-                    if constexpr (OUT == kWeights) x = fmaf(-sink.rate, x, sink.keep * Elem<T>::load(out + e));
-                    if constexpr (OUT == kMasters) master[e] = x = fmaf(-sink.rate, x, sink.keep * master[e]);
-                    Elem<T>::store(out + e, x);
+                    put<T, OUT>(sink, out + e, OUT == kMasters ? master + e : nullptr, v[e] * (1.f / (kX * kP)));
                 }
             } else {
                 // (what lies past a row's numbers is zero: the rows that do not exist were read as zeros)
@@ -251,6 +256,156 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
                 }
             }
         }
+}
+
+// ---- small blocks: the whole of it in one launch ----
+
+// A block of up to S x S, zeros around it, in a workgroup of four waves: X both ways round, A and P stay in LDS as operands (rows of S / 32
+// steps of 128 bytes, a step of all rows after the other, 16-byte piece u of row r in place u ^ (r % 8)), the sums in registers.  What is
+// beside A on the other side of P, where m > n, is zeros times a: the same X'.  Bound by latency: three products and four barriers a step.
+template <int S>
+struct Small {
+    static constexpr int STEPS = S / 32, SIZE = S * STEPS * 128, T = S / 32;  // T x T tiles of 16 x 16 a wave
+    static __device__ __forceinline__ int at(int row, int k, int plane)
+    {
+        return (k >> 5) * (S * 128) + row * 128 + 16 * ((4 * plane + ((k & 31) >> 3)) ^ (row & 7)) + 2 * (k & 7);
+    }
+};
+
+template <int S>
+__device__ __forceinline__ void small_product(const unsigned char* a, const unsigned char* b, f32x4 (&acc)[S / 32][S / 32])
+{
+    using K = Small<S>;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, at0 = 16 * ((lane >> 4) ^ (lane & 7)), at1 = at0 ^ 64;
+    const unsigned char *pa = a + ((wave >> 1) * (S / 2) + r16) * 128, *pb = b + ((wave & 1) * (S / 2) + r16) * 128;
+#pragma unroll
+    for (int i = 0; i < K::T; ++i)
+#pragma unroll
+        for (int j = 0; j < K::T; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < K::STEPS; ++s) {
+        u32x4 b0[K::T], b1[K::T];
+#pragma unroll
+        for (int j = 0; j < K::T; ++j) {
+            b0[j] = lds128(pb + s * S * 128 + j * 2048 + at0);
+            b1[j] = lds128(pb + s * S * 128 + j * 2048 + at1);
+        }
+#pragma unroll
+        for (int i = 0; i < K::T; ++i) {
+            const u32x4 a0 = lds128(pa + s * S * 128 + i * 2048 + at0), a1 = lds128(pa + s * S * 128 + i * 2048 + at1);
+#pragma unroll
+            for (int j = 0; j < K::T; ++j) acc[i][j] = nt_step<kF16x2>(a0, a1, b0[j], b1[j], acc[i][j]);
+        }
+    }
+}
+
+template <int S, typename G, bool MUON, typename T, Out OUT>
+__global__ __launch_bounds__(256) void ortho_small_kernel(Source src, Sink sink, float ca, float cb, float cc, int steps, float eps)
+{
+    using K = Small<S>;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    __shared__ double part[4];
+    unsigned char *x = lds, *xt = lds + K::SIZE, *gram = lds + 2 * K::SIZE, *poly = lds + 3 * K::SIZE;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = src.m, n = src.n;
+    const int tensor = blockIdx.x / src.blocks;
+    const int64_t base = (int64_t)((int)blockIdx.x - tensor * src.blocks) * m * n;
+    const G* g = (const G*)src.g[tensor] + base;
+    float* v = MUON ? src.v[tensor] + base : nullptr;
+    // four rows of four numbers a thread (S = 64; 32: one): the numbers that leave together lie along k of one operand or the other
+    constexpr int Q = S * S / 1024;
+    float u[Q][4];
+    double sum = 0;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int i = (tid + 256 * q) / (S / 4), j = (tid + 256 * q) % (S / 4) * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            u[q][e] = 0.f;
+            if (i < m && j + e < n) {
+                const int p = i * n + j + e;
+                const float gi = Elem<G>::load(g + p);
+                u[q][e] = gi;
+                if constexpr (MUON) {
+                    const float vi = fmaf(src.momentum, v[p], gi);
+                    v[p] = vi;
+                    u[q][e] = src.nesterov ? fmaf(src.momentum, vi, gi) : vi;
+                }
+            }
+            sum += (double)u[q][e] * u[q][e];
+        }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    const double by = (double)kX / (sqrt(part[0] + part[1] + part[2] + part[3]) + (double)eps);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int i = (tid + 256 * q) / (S / 4), j = (tid + 256 * q) % (S / 4) * 4;
+        f32x4 w = {(float)(u[q][0] * by), (float)(u[q][1] * by), (float)(u[q][2] * by), (float)(u[q][3] * by)};
+#pragma unroll
+        for (int plane = 0; plane < 2; ++plane) {
+            const u32x2 h = take_plane(w);
+            *reinterpret_cast<u32x2*>(x + K::at(i, j, plane)) = h;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) *reinterpret_cast<uint16_t*>(xt + K::at(j + e, i, plane)) = (uint16_t)(h[e >> 1] >> (16 * (e & 1)));
+        }
+    }
+    __syncthreads();
+    const int a0 = (wave >> 1) * (S / 2) + 4 * (lane >> 4), b0 = (wave & 1) * (S / 2) + (lane & 15);  // first a-row of a lane's four, its b-row
+    f32x4 acc[K::T][K::T], keep[K::T][K::T];
+    for (int step = 0; step < steps; ++step) {
+        small_product<S>(x, x, keep);
+#pragma unroll
+        for (int i = 0; i < K::T; ++i)
+#pragma unroll
+            for (int j = 0; j < K::T; ++j) {
+                f32x4 w = keep[i][j] *= kA / (kX * kX);
+#pragma unroll
+                for (int plane = 0; plane < 2; ++plane) *reinterpret_cast<u32x2*>(gram + K::at(b0 + 16 * j, a0 + 16 * i, plane)) = take_plane(w);
+            }
+        __syncthreads();
+        small_product<S>(gram, gram, acc);
+#pragma unroll
+        for (int i = 0; i < K::T; ++i)
+#pragma unroll
+            for (int j = 0; j < K::T; ++j) {
+                f32x4 w = acc[i][j] * (cc * (kP / (kA * kA))) + keep[i][j] * (cb * (kP / kA));
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (a0 + 16 * i + e == b0 + 16 * j) w[e] = fmaf(ca, kP, w[e]);
+#pragma unroll
+                for (int plane = 0; plane < 2; ++plane) *reinterpret_cast<u32x2*>(poly + K::at(b0 + 16 * j, a0 + 16 * i, plane)) = take_plane(w);
+            }
+        __syncthreads();
+        small_product<S>(poly, xt, acc);
+        if (step + 1 == steps) break;
+        __syncthreads();  // X has been read
+#pragma unroll
+        for (int i = 0; i < K::T; ++i)
+#pragma unroll
+            for (int j = 0; j < K::T; ++j) {
+                f32x4 w = acc[i][j] * (1.f / kP);
+#pragma unroll
+                for (int plane = 0; plane < 2; ++plane) {
+                    const u32x2 h = take_plane(w);
+                    *reinterpret_cast<u32x2*>(xt + K::at(b0 + 16 * j, a0 + 16 * i, plane)) = h;
+                    *reinterpret_cast<u32x2*>(x + K::at(a0 + 16 * i + (lane & 3), (b0 + 16 * j) & ~3, plane)) = change_places(h);
+                }
+            }
+        __syncthreads();
+    }
+    T* out = (T*)sink.out[tensor] + base;
+    float* master = OUT == kMasters ? sink.master[tensor] + base : nullptr;
+#pragma unroll
+    for (int i = 0; i < K::T; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int j = 0; j < K::T; ++j) {
+                const int row = a0 + 16 * i + e, col = b0 + 16 * j;
+                if (row < m && col < n) put<T, OUT>(sink, out + row * n + col, OUT == kMasters ? master + row * n + col : nullptr, acc[i][j][e] * (1.f / (kX * kP)));
+            }
 }
 
 // ---- plan ----
@@ -350,6 +505,19 @@ int steps_of(const OrthoShape& s, const OrthoSteps& k, OrthoArea& a, const Sink&
     return 0;
 }
 
+bool is_small(const OrthoShape& s) { return s.m <= 64 && s.n <= 64; }
+template <typename G, bool MUON, typename T, Out OUT>
+int run_small(const OrthoShape& s, const OrthoSteps& k, const Source& src, const Sink& sink, hipStream_t st)
+{
+    auto go = [&](auto kernel, size_t lds) {
+        if (allow_dynamic_lds((const void*)kernel, lds) != hipSuccess) return -4;
+        kernel<<<(unsigned)s.all(), 256, lds, st>>>(src, sink, k.a, k.b, k.c, k.steps, k.eps);
+        return launched();
+    };
+    if (s.m <= 32 && s.n <= 32) return go(ortho_small_kernel<32, G, MUON, T, OUT>, 4 * Small<32>::SIZE);
+    return go(ortho_small_kernel<64, G, MUON, T, OUT>, 4 * Small<64>::SIZE);
+}
+
 template <typename T, bool MUON>
 int first_operands(const OrthoShape& s, const OrthoSteps& k, const Source& src, const OrthoArea& a, hipStream_t st)
 {
@@ -370,13 +538,14 @@ bool ortho_supported(const OrthoShape& s)
 size_t ortho_workspace(const OrthoShape& s)
 {
     OrthoArea a;
+    if (s.all() && is_small(s)) return 256;  // (none, but a workspace all the same)
     return s.all() ? a.lay(s, nullptr) : 0;
 }
 
 int ortho_run(const OrthoShape& s, const OrthoSteps& k, const void* g, void* x, bool bf16, void* ws, hipStream_t st)
 {
     OrthoArea a;
-    a.lay(s, (char*)ws);
+    if (!is_small(s)) a.lay(s, (char*)ws);
     Source src{};
     src.g[0] = g;
     src.blocks = (int)s.blocks;
@@ -387,6 +556,8 @@ int ortho_run(const OrthoShape& s, const OrthoSteps& k, const void* g, void* x, 
     sink.blocks = (int)s.blocks;
     sink.m = s.m;
     sink.n = s.n;
+    if (is_small(s))
+        return bf16 ? run_small<uint16_t, false, uint16_t, kPlain>(s, k, src, sink, st) : run_small<float, false, float, kPlain>(s, k, src, sink, st);
     if (int rc = bf16 ? first_operands<uint16_t, false>(s, k, src, a, st) : first_operands<float, false>(s, k, src, a, st)) return rc;
     return bf16 ? steps_of<uint16_t, kPlain>(s, k, a, sink, st) : steps_of<float, kPlain>(s, k, a, sink, st);
 }
@@ -395,7 +566,7 @@ int muon_run(const OrthoShape& s, const OrthoSteps& k, const MuonRule& rule, voi
              float* const* masters, bool weights_bf16, bool grads_bf16, void* ws, hipStream_t st)
 {
     OrthoArea a;
-    a.lay(s, (char*)ws);
+    if (!is_small(s)) a.lay(s, (char*)ws);
     Source src{};
     Sink sink{};
     for (int i = 0; i < s.count; ++i) {
@@ -411,6 +582,13 @@ int muon_run(const OrthoShape& s, const OrthoSteps& k, const MuonRule& rule, voi
     src.nesterov = rule.nesterov;
     sink.keep = 1.f - rule.lr * rule.decay;
     sink.rate = rule.lr * rule.scale;
+    if (is_small(s)) {
+        if (masters)
+            return grads_bf16 ? run_small<uint16_t, true, uint16_t, kMasters>(s, k, src, sink, st) : run_small<float, true, uint16_t, kMasters>(s, k, src, sink, st);
+        if (weights_bf16)
+            return grads_bf16 ? run_small<uint16_t, true, uint16_t, kWeights>(s, k, src, sink, st) : run_small<float, true, uint16_t, kWeights>(s, k, src, sink, st);
+        return grads_bf16 ? run_small<uint16_t, true, float, kWeights>(s, k, src, sink, st) : run_small<float, true, float, kWeights>(s, k, src, sink, st);
+    }
     if (int rc = grads_bf16 ? first_operands<uint16_t, true>(s, k, src, a, st) : first_operands<float, true>(s, k, src, a, st)) return rc;
     if (masters) return steps_of<uint16_t, kMasters>(s, k, a, sink, st);
     return weights_bf16 ? steps_of<uint16_t, kWeights>(s, k, a, sink, st) : steps_of<float, kWeights>(s, k, a, sink, st);

@@ -149,6 +149,30 @@ __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const
 #endif
 }
 
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+__device__ __forceinline__ uint32_t pack_f16x2(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2_t)); }
+// Two numbers in binary16 (packed, rounded to nearest), and what that leaves of them.
+__device__ __forceinline__ uint32_t take_f16x2(float& a, float& b)
+{
+    const uint32_t u = pack_f16x2(a, b);
+    const f16x2_t h = __builtin_bit_cast(f16x2_t, u);
+    a = fmaf((float)h[0], -1.f, a);  // (one instruction, exact)
+    b = fmaf((float)h[1], -1.f, b);
+    return u;
+}
+// four numbers as two planes
+struct TwoPlanes {
+    u32x2 p[2];
+};
+__device__ __forceinline__ TwoPlanes split_planes(f32x4 v)
+{
+    float a = v[0], b = v[1], c = v[2], d = v[3];
+    TwoPlanes r;
+    r.p[0] = u32x2{take_f16x2(a, b), take_f16x2(c, d)};
+    r.p[1] = u32x2{pack_f16x2(a, b), pack_f16x2(c, d)};
+    return r;
+}
+
 // Among four lanes (4q .. 4q + 3) with four 16-bit numbers each: lane i gets number i of all four.
 __device__ __forceinline__ u32x2 change_places(u32x2 v)
 {

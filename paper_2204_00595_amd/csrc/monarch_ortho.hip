@@ -24,20 +24,8 @@ constexpr float kX = 0x1p11f, kA = 0x1p11f, kP = 0x1p9f;  // what X, A and P are
 __host__ __device__ __forceinline__ uint32_t row_half(int k) { return (uint32_t)((k + 31) / 32 * 64); }
 __device__ __forceinline__ uint32_t place(uint32_t k, int plane) { return (k >> 5) * 64 + 32 * plane + (k & 31); }
 
-__device__ __forceinline__ uint32_t f16_bits(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 __device__ __forceinline__ float f16_value(uint32_t h) { return (float)__builtin_bit_cast(_Float16, (uint16_t)h); }
 
-// four numbers -> their upper plane (packed); v becomes what that leaves
-__device__ __forceinline__ u32x2 take_plane(f32x4& v)
-{
-    uint32_t h[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        h[e] = f16_bits(v[e]);
-        v[e] -= f16_value(h[e]);
-    }
-    return u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
-}
 // ---- norm, momentum, first operands ----
 
 constexpr int kChunk = 4096;  // numbers of a block that a workgroup adds up
@@ -153,9 +141,10 @@ __global__ __launch_bounds__(256) void ortho_pack_kernel(Source s, const double*
             f32x4 u;
 #pragma unroll
             for (int e = 0; e < 4; ++e) u[e] = way ? tile[c + e][r] : tile[r][c + e];
+            const TwoPlanes h = split_planes(u);
 #pragma unroll
             for (int plane = 0; plane < 2; ++plane)
-                *reinterpret_cast<u32x2*>(to + (int64_t)(row0 + r) * half + place(col0 + c, plane)) = take_plane(u);
+                *reinterpret_cast<u32x2*>(to + (int64_t)(row0 + r) * half + place(col0 + c, plane)) = h.p[plane];
         }
     }
 }
@@ -243,9 +232,10 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
                             if (m + e == n) v[e] = fmaf(p.ca, kP, v[e]);
                     }
                 }
+                const TwoPlanes h = split_planes(v);
 #pragma unroll
                 for (int plane = 0; plane < 2; ++plane) {
-                    const u32x2 u = take_plane(v);
+                    const u32x2 u = h.p[plane];
                     if (in_rows) *reinterpret_cast<u32x2*>(row + place(m, plane)) = u;
                     if constexpr (PART == kNext) {
                         const u32x2 w = change_places(u);
@@ -343,9 +333,10 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(Source src, Sink sink,
     for (int q = 0; q < Q; ++q) {
         const int i = (tid + 256 * q) / (S / 4), j = (tid + 256 * q) % (S / 4) * 4;
         f32x4 w = {(float)(u[q][0] * by), (float)(u[q][1] * by), (float)(u[q][2] * by), (float)(u[q][3] * by)};
+        const TwoPlanes two = split_planes(w);
 #pragma unroll
         for (int plane = 0; plane < 2; ++plane) {
-            const u32x2 h = take_plane(w);
+            const u32x2 h = two.p[plane];
             *reinterpret_cast<u32x2*>(x + K::at(i, j, plane)) = h;
 #pragma unroll
             for (int e = 0; e < 4; ++e) *reinterpret_cast<uint16_t*>(xt + K::at(j + e, i, plane)) = (uint16_t)(h[e >> 1] >> (16 * (e & 1)));
@@ -360,9 +351,9 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(Source src, Sink sink,
         for (int i = 0; i < K::T; ++i)
 #pragma unroll
             for (int j = 0; j < K::T; ++j) {
-                f32x4 w = keep[i][j] *= kA / (kX * kX);
+                const TwoPlanes h = split_planes(keep[i][j] *= kA / (kX * kX));
 #pragma unroll
-                for (int plane = 0; plane < 2; ++plane) *reinterpret_cast<u32x2*>(gram + K::at(b0 + 16 * j, a0 + 16 * i, plane)) = take_plane(w);
+                for (int plane = 0; plane < 2; ++plane) *reinterpret_cast<u32x2*>(gram + K::at(b0 + 16 * j, a0 + 16 * i, plane)) = h.p[plane];
             }
         __syncthreads();
         small_product<S>(gram, gram, acc);
@@ -374,8 +365,9 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(Source src, Sink sink,
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (a0 + 16 * i + e == b0 + 16 * j) w[e] = fmaf(ca, kP, w[e]);
+                const TwoPlanes h = split_planes(w);
 #pragma unroll
-                for (int plane = 0; plane < 2; ++plane) *reinterpret_cast<u32x2*>(poly + K::at(b0 + 16 * j, a0 + 16 * i, plane)) = take_plane(w);
+                for (int plane = 0; plane < 2; ++plane) *reinterpret_cast<u32x2*>(poly + K::at(b0 + 16 * j, a0 + 16 * i, plane)) = h.p[plane];
             }
         __syncthreads();
         small_product<S>(poly, xt, acc);
@@ -385,10 +377,10 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(Source src, Sink sink,
         for (int i = 0; i < K::T; ++i)
 #pragma unroll
             for (int j = 0; j < K::T; ++j) {
-                f32x4 w = acc[i][j] * (1.f / kP);
+                const TwoPlanes two = split_planes(acc[i][j] * (1.f / kP));
 #pragma unroll
                 for (int plane = 0; plane < 2; ++plane) {
-                    const u32x2 h = take_plane(w);
+                    const u32x2 h = two.p[plane];
                     *reinterpret_cast<u32x2*>(xt + K::at(b0 + 16 * j, a0 + 16 * i, plane)) = h;
                     *reinterpret_cast<u32x2*>(x + K::at(a0 + 16 * i + (lane & 3), (b0 + 16 * j) & ~3, plane)) = change_places(h);
                 }

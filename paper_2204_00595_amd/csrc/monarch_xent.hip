@@ -19,15 +19,6 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 __device__ __forceinline__ float log2_fast(float v) { return __builtin_amdgcn_logf(v); }
 
-__device__ __forceinline__ uint16_t f32_to_f16_bits(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
-// the upper plane's number and what it leaves
-__device__ __forceinline__ void split2(float v, uint16_t& hi, uint16_t& lo)
-{
-    const _Float16 h = (_Float16)v;
-    hi = __builtin_bit_cast(uint16_t, h);
-    lo = f32_to_f16_bits(v - (float)h);
-}
-
 // Power of two that brings `top` (the largest finite magnitude) to 2^14 .. 2^15, and its inverse.
 __device__ __forceinline__ float scale_for(float top)
 {
@@ -59,16 +50,15 @@ __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 template <bool PLANES>
 __device__ __forceinline__ void store_planes(uint16_t* at, const float (&v)[8], float up)
 {
-    uint32_t hi[8], lo[8];
+    u32x4 hi, lo;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        uint16_t h, l;
-        split2(v[e] * up, h, l);
-        hi[e] = h;
-        lo[e] = l;
+    for (int e = 0; e < 4; ++e) {
+        float a = v[2 * e] * up, b = v[2 * e + 1] * up;
+        hi[e] = take_f16x2(a, b);
+        lo[e] = pack_f16x2(a, b);
     }
-    *reinterpret_cast<u32x4*>(at) = u32x4{hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16};
-    if constexpr (PLANES) *reinterpret_cast<u32x4*>(at + 32) = u32x4{lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16};
+    *reinterpret_cast<u32x4*>(at) = hi;
+    if constexpr (PLANES) *reinterpret_cast<u32x4*>(at + 32) = lo;
 }
 
 constexpr int kTops = 1024;  // workgroups, at most, that leave the largest magnitude they met
@@ -411,14 +401,8 @@ __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const f
     }
     // plane `plane` of four numbers times `by`
     auto four = [&](const f32x4& s, float by, int plane) {
-        uint32_t h[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float v = s[e] * by;
-            const _Float16 f = (_Float16)v;
-            h[e] = plane ? f32_to_f16_bits(v - (float)f) : (uint32_t)__builtin_bit_cast(uint16_t, f);
-        }
-        return u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+        if constexpr (C::PL == 2) return split_planes(s * by).p[plane];
+        return u32x2{pack_f16x2(s[0] * by, s[1] * by), pack_f16x2(s[2] * by, s[3] * by)};
     };
     // 16-byte piece u of LDS row r in place u ^ (r % 16), of the other way round u ^ (r % 8)
 #pragma unroll

@@ -3,8 +3,9 @@
 // which moves every singular value s to a s + b s^3 + c s^5 and leaves the singular vectors.  A is taken on the shorter side, r = min(m, n);
 // below X is r x c (the transpose of the block where it is higher than wide).
 //
-// Three products a step, all along the rows of their operands (monarch_nt.h): A = X X^T, P = a I + b A + c A A^T (A is symmetric), X' = P X
-// with X kept both ways round.  Operands are binary16 numbers times a power of two, in two planes: entries of X and A are below 2, those
+// Three products a step (monarch_nt.h): A = X X^T, P = a I + b A + c A A^T (A is symmetric: of the tiles of A and P those on and below the
+// diagonal are computed), X' = P X.  X lies transposed, c rows of r numbers: the first product reads it across, the last along its rows,
+// and writes the next one so.  Operands are binary16 numbers times a power of two, in two planes: entries of X and A are below 2, those
 // of P below |a| + 2 |b| + 4 |c|, and 22 bits of each are kept (five steps of the 3.4445, -4.7750, 2.0315 polynomial lose 2.5e-7 of the
 // result's norm, fp32 products 1e-6 to 2e-6).  bf16 gradients take the same: with one plane (11 bits) the result would be 1.0e-3 to
 // 1.5e-3 off beside its own rounding of 1.7e-3, and far more where a few directions stand out, since small singular values grow up to
@@ -92,11 +93,9 @@ __global__ __launch_bounds__(256) void ortho_norm_kernel(Source s, double* __res
     if (threadIdx.x == 0) part[(int64_t)block * gridDim.x + blockIdx.x] = wave[0] + wave[1] + wave[2] + wave[3];
 }
 
-// The update over its norm as operands, rows as they are (along: m rows of n) and columns (across: n rows of m), 64 x 64 at a time; zeros up to
-// whole steps.
-template <typename T, bool MUON>
-__global__ __launch_bounds__(256) void ortho_pack_kernel(Source s, const double* __restrict__ part, int parts, float eps,
-                                                         uint16_t* __restrict__ along, uint16_t* __restrict__ across)
+// The update over its norm as an operand, 64 x 64 at a time: its rows (TURN: its columns), zeros up to whole pieces.
+template <typename T, bool MUON, bool TURN>
+__global__ __launch_bounds__(256) void ortho_pack_kernel(Source s, const double* __restrict__ part, int parts, float eps, uint16_t* __restrict__ to)
 {
     __shared__ float tile[64][65];
     __shared__ double wave[4];
@@ -126,26 +125,19 @@ __global__ __launch_bounds__(256) void ortho_pack_kernel(Source s, const double*
         tile[4 * k + (tid >> 6)][tid & 63] = u;
     }
     __syncthreads();
-    const uint32_t half_n = row_half(s.n), half_m = row_half(s.m);
-    along += (int64_t)block * s.m * half_n;
-    across += (int64_t)block * s.n * half_m;
+    const int row0 = TURN ? j0 : i0, col0 = TURN ? i0 : j0, rows = TURN ? s.n : s.m;
+    const uint32_t half = row_half(TURN ? s.m : s.n);
+    to += (int64_t)block * rows * half;
 #pragma unroll
-    for (int way = 0; way < 2; ++way) {
-        const int row0 = way ? j0 : i0, col0 = way ? i0 : j0, rows = way ? s.n : s.m;
-        const uint32_t half = way ? half_m : half_n;
-        uint16_t* to = way ? across : along;
+    for (int k = 0; k < 4; ++k) {
+        const int piece = 256 * k + tid, r = piece >> 4, c = (piece & 15) * 4;
+        if (row0 + r >= rows || (uint32_t)(col0 + c) * 2 >= half) continue;
+        f32x4 u;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int piece = 256 * k + tid, r = piece >> 4, c = (piece & 15) * 4;
-            if (row0 + r >= rows || (uint32_t)(col0 + c) * 2 >= half) continue;
-            f32x4 u;
+        for (int e = 0; e < 4; ++e) u[e] = TURN ? tile[c + e][r] : tile[r][c + e];
+        const TwoPlanes h = split_planes(u);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) u[e] = way ? tile[c + e][r] : tile[r][c + e];
-            const TwoPlanes h = split_planes(u);
-#pragma unroll
-            for (int plane = 0; plane < 2; ++plane)
-                *reinterpret_cast<u32x2*>(to + (int64_t)(row0 + r) * half + place(col0 + c, plane)) = h.p[plane];
-        }
+        for (int plane = 0; plane < 2; ++plane) *reinterpret_cast<u32x2*>(to + (int64_t)(row0 + r) * half + place(col0 + c, plane)) = h.p[plane];
     }
 }
 
@@ -154,12 +146,13 @@ __global__ __launch_bounds__(256) void ortho_pack_kernel(Source s, const double*
 enum Part { kGram, kPoly, kNext, kLast };
 
 struct Product {
-    const uint16_t *a, *b;  // operands of all blocks: rows of them, 16-bit numbers a row
-    int a_rows, b_rows;
-    uint32_t half;          // of both
-    int tiles_a, tiles_b, blocks;
-    uint16_t *rows, *cols;  // results as operands: row b of them, and (kNext) row a of them
-    uint32_t rows_half, cols_half;
+    const uint16_t *a, *b;  // operands of all blocks
+    int a_rows, b_rows;     // rows of the result that each brings (kGram: columns of X)
+    int k_rows;             // kGram: rows of X
+    uint32_t half;          // 16-bit numbers of a row of both
+    int tiles_a, tiles_b, tiles, blocks;  // tiles of a block: all, or on and below the diagonal
+    uint16_t* rows;         // the result as an operand: row b of it
+    uint32_t rows_half;
     const uint16_t* gram;   // kPoly
     float ca, cb, cc;
 };
@@ -180,18 +173,41 @@ __device__ __forceinline__ void put(const Sink& sink, T* out, float* master, flo
     Elem<T>::store(out, x);
 }
 
+template <typename T, Out OUT>
+__device__ __forceinline__ void put4(const Sink& sink, T* out, float* master, f32x4 x)
+{
+    if constexpr (OUT == kWeights) x = sink.keep * load4(out) - sink.rate * x;
+    if constexpr (OUT == kMasters) *reinterpret_cast<f32x4*>(master) = x = sink.keep * load4(master) - sink.rate * x;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(out) = x;
+    else *reinterpret_cast<u32x2*>(out) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+}
+
 template <typename C, Part PART, typename T, Out OUT>
 __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Sink sink)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    constexpr bool HALF = PART == kGram || PART == kPoly;  // (symmetric)
     // a block's tiles lie together on an XCD
-    const int tiles = p.tiles_a * p.tiles_b, total = tiles * p.blocks, each = (total + 7) >> 3;
+    const int total = p.tiles * p.blocks, each = (total + 7) >> 3;
     const int t = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= each || t >= total) return;
-    const int block = t / tiles, in = t - block * tiles, tb = in / p.tiles_a, ta = in - tb * p.tiles_a;
-    const NtOperand a{p.a + (int64_t)block * p.a_rows * p.half, p.a_rows, p.half * 2}, b{p.b + (int64_t)block * p.b_rows * p.half, p.b_rows, p.half * 2};
+    const int block = t / p.tiles, in = t - block * p.tiles;
+    int ta, tb;
+    if constexpr (HALF) {
+        for (ta = 0, tb = in; tb > ta; ++ta) tb -= ta + 1;  // rows of 1, 2, 3, .. tiles
+    } else {
+        tb = in / p.tiles_a;
+        ta = in - tb * p.tiles_a;
+    }
     f32x4 acc[C::TI][C::TJ];
-    nt_product<C>(a, (int64_t)ta * C::BM, b, (int64_t)tb * C::BN, 0, (int)(p.half / 64), lds, acc);
+    if constexpr (PART == kGram) {
+        const NtOperand x{p.a + (int64_t)block * p.k_rows * p.half, p.k_rows, p.half * 2};
+        nt_product<C, false, true, true>(x, (int64_t)ta * C::BM, x, (int64_t)tb * C::BN, 0, (p.k_rows + 31) / 32, lds, acc);
+    } else {
+        const NtOperand a{p.a + (int64_t)block * p.a_rows * p.half, p.a_rows, p.half * 2};
+        const NtOperand b{p.b + (int64_t)block * p.b_rows * p.half, p.b_rows, p.half * 2};
+        nt_product<C>(a, (int64_t)ta * C::BM, b, (int64_t)tb * C::BN, 0, (int)(p.half / 64), lds, acc);
+    }
     const int lane = threadIdx.x & 63;
     const int m0 = ta * C::BM + C::row0() + 4 * (lane >> 4), n0 = tb * C::BN + C::col0() + (lane & 15);
 #pragma unroll
@@ -201,20 +217,22 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
             const int m = m0 + 16 * i, n = n0 + 16 * j;
             f32x4 v = acc[i][j];
             if constexpr (PART == kLast) {
-                if (n >= p.b_rows) continue;
+                if (n >= p.b_rows || m >= p.a_rows) continue;
                 const int tensor = block / sink.blocks;
                 const int64_t at = (int64_t)(block - tensor * sink.blocks) * sink.m * sink.n + (int64_t)n * sink.n + m;
                 T* out = (T*)sink.out[tensor] + at;
                 float* master = OUT == kMasters ? sink.master[tensor] + at : nullptr;
+                v *= 1.f / (kX * kP);
+                if ((sink.n & 3) == 0) {
+                    put4<T, OUT>(sink, out, master, v);
+                } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (m + e >= p.a_rows) break;
-                    put<T, OUT>(sink, out + e, OUT == kMasters ? master + e : nullptr, v[e] * (1.f / (kX * kP)));
+                    for (int e = 0; e < 4; ++e)
+                        if (m + e < p.a_rows) put<T, OUT>(sink, out + e, OUT == kMasters ? master + e : nullptr, v[e]);
                 }
             } else {
                 // (what lies past a row's numbers is zero: the rows that do not exist were read as zeros)
                 const bool in_rows = n < p.b_rows && (uint32_t)m * 2 < p.rows_half;
-                uint16_t* row = p.rows + ((int64_t)block * p.b_rows + n) * p.rows_half;
                 if constexpr (PART == kGram) v *= kA / (kX * kX);
                 if constexpr (PART == kNext) v *= 1.f / kP;
                 if constexpr (PART == kPoly) {
@@ -232,16 +250,20 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
                             if (m + e == n) v[e] = fmaf(p.ca, kP, v[e]);
                     }
                 }
+                if constexpr (PART == kGram) {  // (across, the numbers past a row's last are the next row's)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = m + e < p.a_rows ? v[e] : 0.f;
+                }
                 const TwoPlanes h = split_planes(v);
 #pragma unroll
                 for (int plane = 0; plane < 2; ++plane) {
-                    const u32x2 u = h.p[plane];
-                    if (in_rows) *reinterpret_cast<u32x2*>(row + place(m, plane)) = u;
-                    if constexpr (PART == kNext) {
-                        const u32x2 w = change_places(u);
+                    if (in_rows) *reinterpret_cast<u32x2*>(p.rows + ((int64_t)block * p.b_rows + n) * p.rows_half + place(m, plane)) = h.p[plane];
+                    if constexpr (HALF) {
+                        // the other side of the diagonal
+                        const u32x2 w = change_places(n < p.b_rows ? h.p[plane] : u32x2{0, 0});
                         const int r = m + (lane & 3), c = n & ~3;
-                        if (r < p.a_rows && (uint32_t)c * 2 < p.cols_half)
-                            *reinterpret_cast<u32x2*>(p.cols + ((int64_t)block * p.a_rows + r) * p.cols_half + place(c, plane)) = w;
+                        if (ta != tb && r < p.a_rows && (uint32_t)c * 2 < p.rows_half)
+                            *reinterpret_cast<u32x2*>(p.rows + ((int64_t)block * p.a_rows + r) * p.rows_half + place(c, plane)) = w;
                     }
                 }
             }
@@ -405,8 +427,8 @@ __global__ __launch_bounds__(256) void ortho_small_kernel(Source src, Sink sink,
 struct OrthoArea {
     double* part;
     int parts;
-    uint16_t *xr[2], *xt[2], *gram, *poly;
-    uint32_t half_r, half_c;
+    uint16_t *x[2], *gram, *poly;
+    uint32_t half;  // 16-bit numbers of a row of X (transposed), A and P
     int r, c;
     size_t lay(const OrthoShape& s, char* base)
     {
@@ -418,16 +440,12 @@ struct OrthoArea {
         };
         r = s.m < s.n ? s.m : s.n;
         c = s.m < s.n ? s.n : s.m;
-        half_r = row_half(r);
-        half_c = row_half(c);
+        half = row_half(r);
         parts = (int)(((int64_t)s.m * s.n + kChunk - 1) / kChunk);
         part = (double*)take(s.all() * parts * sizeof(double));
-        for (int i = 0; i < 2; ++i) {
-            xr[i] = (uint16_t*)take((size_t)s.all() * r * half_c * 2);
-            xt[i] = (uint16_t*)take((size_t)s.all() * c * half_r * 2);
-        }
-        gram = (uint16_t*)take((size_t)s.all() * r * half_r * 2);
-        poly = (uint16_t*)take((size_t)s.all() * r * half_r * 2);
+        for (int i = 0; i < 2; ++i) x[i] = (uint16_t*)take((size_t)s.all() * c * half * 2);
+        gram = (uint16_t*)take((size_t)s.all() * r * half * 2);
+        poly = (uint16_t*)take((size_t)s.all() * r * half * 2);
         return used;
     }
 };
@@ -440,16 +458,18 @@ int run_product(Product p, const Sink& sink, hipStream_t st)
     if (allow_dynamic_lds((const void*)ortho_product_kernel<C, PART, T, OUT>, C::LDS_BYTES) != hipSuccess) return -4;
     p.tiles_a = (p.a_rows + C::BM - 1) / C::BM;
     p.tiles_b = (p.b_rows + C::BN - 1) / C::BN;
-    const unsigned grid = (unsigned)((p.tiles_a * p.tiles_b * p.blocks + 7) / 8 * 8);
+    p.tiles = PART == kGram || PART == kPoly ? p.tiles_a * (p.tiles_a + 1) / 2 : p.tiles_a * p.tiles_b;
+    const unsigned grid = (unsigned)((p.tiles * p.blocks + 7) / 8 * 8);
     ortho_product_kernel<C, PART, T, OUT><<<grid, C::THREADS, C::LDS_BYTES, st>>>(p, sink);
     return launched();
 }
 template <Part PART, typename T, Out OUT>
 int product(const Product& p, const Sink& sink, hipStream_t st)
 {
-    using Low = NtTile<64, 64, 32, 32, kF16x2, 4>;
+    using Low = NtTile<64, 64, 32, 32, kF16x2>;
     using Mid = NtTile<128, 128, 64, 64, kF16x2>;
-    const int64_t mid = (int64_t)((p.a_rows + 127) / 128) * ((p.b_rows + 127) / 128) * p.blocks;
+    const int64_t a = (p.a_rows + 127) / 128, b = (p.b_rows + 127) / 128;
+    const int64_t mid = (PART == kGram || PART == kPoly ? a * (a + 1) / 2 : a * b) * p.blocks;
     return mid >= 256 ? run_product<Mid, PART, T, OUT>(p, sink, st) : run_product<Low, PART, T, OUT>(p, sink, st);
 }
 
@@ -459,31 +479,26 @@ int steps_of(const OrthoShape& s, const OrthoSteps& k, OrthoArea& a, const Sink&
     const bool tall = s.m > s.n;
     Product p{};
     p.blocks = (int)s.all();
+    p.half = p.rows_half = a.half;
     p.ca = k.a;
     p.cb = k.b;
     p.cc = k.c;
     for (int i = 0; i < k.steps; ++i) {
-        const int at = i & 1;
         Product gram = p, poly = p, next = p;
-        gram.a = gram.b = a.xr[at];
+        gram.a = a.x[i & 1];
         gram.a_rows = gram.b_rows = poly.a_rows = poly.b_rows = a.r;
-        gram.half = a.half_c;
+        gram.k_rows = a.c;
         gram.rows = a.gram;
-        gram.rows_half = poly.half = poly.rows_half = a.half_r;
         poly.a = poly.b = poly.gram = a.gram;
         poly.rows = a.poly;
         if (int rc = product<kGram, uint16_t, kPlain>(gram, sink, st)) return rc;
         if (int rc = product<kPoly, uint16_t, kPlain>(poly, sink, st)) return rc;
-        next.half = a.half_r;
         next.a = a.poly;
         next.a_rows = a.r;
-        next.b = a.xt[at];
+        next.b = a.x[i & 1];
         next.b_rows = a.c;
         if (i + 1 < k.steps) {
-            next.rows = a.xt[at ^ 1];
-            next.rows_half = a.half_r;
-            next.cols = a.xr[at ^ 1];
-            next.cols_half = a.half_c;
+            next.rows = a.x[(i + 1) & 1];
             if (int rc = product<kNext, uint16_t, kPlain>(next, sink, st)) return rc;
         } else {
             // out[b][a]: the side that lies last in memory is a
@@ -516,8 +531,9 @@ int first_operands(const OrthoShape& s, const OrthoSteps& k, const Source& src, 
     const bool tall = s.m > s.n;
     const unsigned all = (unsigned)s.all();
     ortho_norm_kernel<T, MUON><<<dim3((unsigned)a.parts, all), 256, 0, st>>>(src, a.part);
-    ortho_pack_kernel<T, MUON><<<dim3((s.m + 63) / 64, (s.n + 63) / 64, all), 256, 0, st>>>(src, a.part, a.parts, k.eps, tall ? a.xt[0] : a.xr[0],
-                                                                                               tall ? a.xr[0] : a.xt[0]);
+    const dim3 tiles((s.m + 63) / 64, (s.n + 63) / 64, all);
+    if (tall) ortho_pack_kernel<T, MUON, false><<<tiles, 256, 0, st>>>(src, a.part, a.parts, k.eps, a.x[0]);
+    else ortho_pack_kernel<T, MUON, true><<<tiles, 256, 0, st>>>(src, a.part, a.parts, k.eps, a.x[0]);
     return launched();
 }
 

@@ -3,11 +3,12 @@
 // and the sum of the exponentials of each 256 (or fewer) entries of the vocabulary a row, the backward computes the logits a second time
 // and holds G for a piece of the vocabulary.
 //
-// Every product is along the rows of its operands (monarch_nt.h), so what a product contracts over lies last: dx takes W^T, dW takes x^T
-// and G^T, laid out here.  The logits take bf16 operands as they are and fp32 operands as two binary16 planes: 22 bits of each number at
-// three matrix products instead of the six that three bf16 planes need; powers of two, one for each row that is not contracted over, keep
-// them in binary16's range.  G, W^T and x^T are binary16 times a power of two for both types, one plane beside bf16 tensors (whose 8 bits
-// fit it whole, so that G keeps 11 bits where bf16 would leave 8) and two beside fp32 ones.
+// The logits take bf16 operands as they are and fp32 operands as two binary16 planes (monarch_nt.h): 22 bits of each number at three matrix
+// products instead of the six that three bf16 planes need; powers of two, one for each row, keep them in binary16's range.  G and what it
+// is multiplied with are binary16 times a power of two for both types, one plane beside bf16 tensors (whose 8 bits fit it whole, so that G
+// keeps 11 bits where bf16 would leave 8) and two beside fp32 ones.  G exists once, with the vocabulary last, and without the upstream
+// gradient: dx takes that row by row at its end, dW takes it with x.  dx = G W contracts over the vocabulary and has W^T laid out for
+// it; dW = G^T x contracts over the rows of x, takes x^T, and reads G across them.
 #include "monarch_xent.h"
 #include "monarch_device.h"
 #include "monarch_nt.h"
@@ -75,7 +76,7 @@ __device__ __forceinline__ float largest_of(const float* __restrict__ v, int n)
     return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
 }
 
-// A wave a row: the largest magnitude of the rows with dl != 0 (dl may be null: all) -> tops[workgroup].  With `dst`, the rows as an operand too.
+// A wave a row: the largest magnitude of src, or with dl of dl[row] src -> tops[workgroup].  With `dst`, the rows as an operand too.
 // bf16: copied, zeros up to whole steps.  fp32: two planes, the row's inverse power of two in inv[row].
 template <typename T>
 __global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, int64_t rows, int width, uint16_t* __restrict__ dst,
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, in
             for (int k = 4 * quads + lane; k < width; k += 64) m = fmaxf(m, finite_magnitude(Elem<T>::load(s + k)));
         }
         m = wave_all(m, max_of);
-        if (!(dl && dl[row] == 0.f)) all = fmaxf(all, m);
+        all = fmaxf(all, dl ? finite_magnitude(dl[row]) * m : m);
         if (!dst) continue;
         uint16_t* d = dst + row * (int64_t)row_half;
         if constexpr (sizeof(T) == 2) {
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, in
 }
 
 // Columns of src (rows x width) as rows of an operand of binary16 planes, 64 x 64 at a time, times the power of two for the largest of
-// tops[0 .. n_tops), which goes to *top.  `dl` (may be null): rows with dl = 0 count as zeros, whatever they hold.
+// tops[0 .. n_tops), which goes to *top.  `dl` (may be null): each row times its dl; rows with dl = 0 count as zeros, whatever they hold.
 template <typename T>
 __global__ __launch_bounds__(256) void columns_kernel(const T* __restrict__ src, int64_t rows, int width, uint16_t* __restrict__ dst,
                                                       uint32_t row_half, const float* __restrict__ dl, const float* __restrict__ tops, int n_tops,
@@ -159,16 +160,18 @@ __global__ __launch_bounds__(256) void columns_kernel(const T* __restrict__ src,
         for (int i = 0; i < 2; ++i) {
             const int r = i * 32 + (tid >> 3), c = (tid & 7) * 8;
             u32x4 u = {0, 0, 0, 0};
-            if (k0 + r < rows && c0 + c < width && !(dl && dl[k0 + r] == 0.f)) u = ldg128(src + (k0 + r) * width + c0 + c);
+            const float by = dl && k0 + r < rows ? dl[k0 + r] : 1.f;
+            if (k0 + r < rows && c0 + c < width && by != 0.f) u = ldg128(src + (k0 + r) * width + c0 + c);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) tile[r][c + e] = __uint_as_float(e & 1 ? u[e >> 1] & 0xffff0000u : u[e >> 1] << 16);
+            for (int e = 0; e < 8; ++e) tile[r][c + e] = by * __uint_as_float(e & 1 ? u[e >> 1] & 0xffff0000u : u[e >> 1] << 16);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int r = i * 4 + (tid >> 6), c = tid & 63;
             float v = 0.f;
-            if (k0 + r < rows && c0 + c < width && !(dl && dl[k0 + r] == 0.f)) v = Elem<T>::load(src + (k0 + r) * width + c0 + c);
+            const float by = dl && k0 + r < rows ? dl[k0 + r] : 1.f;
+            if (k0 + r < rows && c0 + c < width && by != 0.f) v = by * Elem<T>::load(src + (k0 + r) * width + c0 + c);
             tile[r][c] = v;
         }
     }
@@ -329,40 +332,27 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2* __restrict_
 
 // ---- backward ----
 
-// Upstream gradient of each row -> dl: zero where ignored, NaN where the target is none.  out[0]: the largest magnitude.
-__global__ __launch_bounds__(1024) void xent_upstream_kernel(const float* __restrict__ dloss, int64_t stride, const float* __restrict__ divisor,
-                                                             const int64_t* __restrict__ target, int64_t ignore, int vocab, int64_t rows,
-                                                             float* __restrict__ dl, float* __restrict__ out)
+// Upstream gradient of each row -> dl: zero where ignored, NaN where the target is none.
+__global__ __launch_bounds__(256) void xent_upstream_kernel(const float* __restrict__ dloss, int64_t stride, const float* __restrict__ divisor,
+                                                            const int64_t* __restrict__ target, int64_t ignore, int vocab, int64_t rows,
+                                                            float* __restrict__ dl)
 {
-    __shared__ float part[16];
-    const float by = divisor ? 1.f / *divisor : 1.f;
-    float m = 0.f;
-    for (int64_t i = threadIdx.x; i < rows; i += 1024) {
-        const int64_t at = target[i];
-        float g = dloss[i * stride] * by;
-        if (at == ignore) g = 0.f;
-        else if (at < 0 || at >= vocab) g = __builtin_nanf("");
-        dl[i] = g;
-        m = fmaxf(m, finite_magnitude(g));
-    }
-    m = wave_all(m, max_of);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 16; ++i) m = fmaxf(m, part[i]);
-        *out = m;
-    }
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows) return;
+    const int64_t at = target[i];
+    float g = dloss[i * stride] * (divisor ? 1.f / *divisor : 1.f);
+    if (at == ignore) g = 0.f;
+    else if (at < 0 || at >= vocab) g = __builtin_nanf("");
+    dl[i] = g;
 }
 
-constexpr float kG = 0x1p14f;  // what exp(l - lse) - [v = target] is stored times where the upstream gradient is left out
+constexpr float kG = 0x1p14f;  // what exp(l - lse) - [v = target] is stored times
 
-// G of a piece of the vocabulary as operands of binary16 planes: once with the vocabulary last and without the upstream gradient, which dx
-// takes row by row (g), and once with the rows of x last and with it, times the power of two for the largest one (gt).  Both leave by
-// way of LDS in runs of 64 bytes and more.  Entries and rows that do not exist are written as zeros.
+// G of a piece of the vocabulary as an operand of binary16 planes, without the upstream gradient; leaves by way of LDS in runs of 64 bytes and
+// more.  Entries and rows that do not exist, and rows that do not count, are written as zeros.
 template <typename C, bool TAIL>
 __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const float* __restrict__ lse, const float* __restrict__ dl,
-                                                               const float* __restrict__ dl_top, uint16_t* __restrict__ g, uint32_t g_half,
-                                                               uint16_t* __restrict__ gt, uint32_t gt_half)
+                                                               uint16_t* __restrict__ g, uint32_t g_half)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int tv, tt;
@@ -373,14 +363,12 @@ __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const f
     const int tid = threadIdx.x, lane = tid & 63;
     const int vr = C::row0() + 4 * (lane >> 4), tc = C::col0() + (lane & 15);
     const int left = p.vocab - v0 - vr < C::BM ? (int)(p.vocab - v0) - vr : C::BM;
-    const float up = scale_for(*dl_top);
-    float d[C::TJ];
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j) {
         const int64_t t = t0 + tc + 16 * j;
         const bool row = t < p.rows;
         const float ls = row ? lse[t] : 0.f;
-        d[j] = row ? dl[t] * up : 0.f;
+        const bool counts = row && dl[t] != 0.f;  // (NaN counts)
 #pragma unroll
         for (int i = 0; i < C::TI; ++i)
 #pragma unroll
@@ -392,74 +380,50 @@ __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const f
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] = at == 16 * i + e ? acc[i][j][e] - 1.f : acc[i][j][e];
         }
-        if (__any(d[j] == 0.f) || left < C::WM) {  // rows that do not count, entries that do not exist
+        if (__any(!counts) || left < C::WM) {  // rows that do not count, entries that do not exist
 #pragma unroll
             for (int i = 0; i < C::TI; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = d[j] == 0.f || 16 * i + e >= left ? 0.f : acc[i][j][e];
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = !counts || 16 * i + e >= left ? 0.f : acc[i][j][e];
         }
     }
-    // plane `plane` of four numbers times `by`
-    auto four = [&](const f32x4& s, float by, int plane) {
-        if constexpr (C::PL == 2) return split_planes(s * by).p[plane];
-        return u32x2{pack_f16x2(s[0] * by, s[1] * by), pack_f16x2(s[2] * by, s[3] * by)};
-    };
-    // 16-byte piece u of LDS row r in place u ^ (r % 16), of the other way round u ^ (r % 8)
+    // 16-byte piece u of LDS row r in place u ^ (r % 16)
 #pragma unroll
     for (int plane = 0; plane < C::PL; ++plane) {
-        if (g) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < C::TI; ++i)
-#pragma unroll
-                for (int j = 0; j < C::TJ; ++j) {
-                    const int r = tc + 16 * j, e = vr + 16 * i;
-                    *reinterpret_cast<u32x2*>(lds + r * (2 * C::BM) + 16 * ((e >> 3) ^ (r & 15)) + 2 * (e & 4)) = four(acc[i][j], kG, plane);
-                }
-            __syncthreads();
-            for (int at = tid; at < C::BN * (C::BM / 8); at += C::THREADS) {
-                const int r = at / (C::BM / 8), u = at % (C::BM / 8);
-                const int64_t k = (int64_t)tv * C::BM + 8 * u;
-                uint16_t* to = g + (t0 + r) * (int64_t)g_half + (C::PL == 1 ? k : (k >> 5) * 64 + 32 * plane + (k & 31));
-                *reinterpret_cast<u32x4*>(to) = lds128(lds + r * (2 * C::BM) + 16 * (u ^ (r & 15)));
-            }
-        }
-        if (!gt) continue;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < C::TI; ++i)
 #pragma unroll
             for (int j = 0; j < C::TJ; ++j) {
-                const int r = vr + 16 * i + (lane & 3), e = C::col0() + 16 * j + (lane & 12);
-                *reinterpret_cast<u32x2*>(lds + r * (2 * C::BN) + 16 * ((e >> 3) ^ (r & 7)) + 2 * (e & 4)) =
-                    change_places(four(acc[i][j], d[j], plane));
+                const int r = tc + 16 * j, e = vr + 16 * i;
+                const f32x4 s = acc[i][j] * kG;
+                u32x2 four;
+                if constexpr (C::PL == 2) four = split_planes(s).p[plane];
+                else four = u32x2{pack_f16x2(s[0], s[1]), pack_f16x2(s[2], s[3])};
+                *reinterpret_cast<u32x2*>(lds + r * (2 * C::BM) + 16 * ((e >> 3) ^ (r & 15)) + 2 * (e & 4)) = four;
             }
         __syncthreads();
-        for (int at = tid; at < C::BM * (C::BN / 8); at += C::THREADS) {
-            const int r = at / (C::BN / 8), u = at % (C::BN / 8);
-            const int64_t k = t0 + 8 * u;
-            uint16_t* to = gt + ((int64_t)tv * C::BM + r) * gt_half + (C::PL == 1 ? k : (k >> 5) * 64 + 32 * plane + (k & 31));
-            *reinterpret_cast<u32x4*>(to) = lds128(lds + r * (2 * C::BN) + 16 * (u ^ (r & 7)));
+        for (int at = tid; at < C::BN * (C::BM / 8); at += C::THREADS) {
+            const int r = at / (C::BM / 8), u = at % (C::BM / 8);
+            const int64_t k = (int64_t)tv * C::BM + 8 * u;
+            uint16_t* to = g + (t0 + r) * (int64_t)g_half + (C::PL == 1 ? k : (k >> 5) * 64 + 32 * plane + (k & 31));
+            *reinterpret_cast<u32x4*>(to) = lds128(lds + r * (2 * C::BM) + 16 * (u ^ (r & 15)));
         }
     }
 }
 
-// What a product of two operands of planes is times: the inverse powers of two of both, and for dx each row's upstream gradient.
+// What a product of G and an operand of planes is times: the inverse powers of two of both, and for dx each row's upstream gradient.
 struct Unscale {
-    const float *top_a, *top_b;  // top_b null: kG alone
-    const float* row;            // of the rows of b (may be null)
-    // two factors (their product alone may be out of range)
-    __device__ __forceinline__ f32x2 factors() const
-    {
-        return f32x2{inverse_power(scale_for(*top_a)), top_b ? inverse_power(scale_for(*top_b)) : 1.f / kG};
-    }
+    const float* top;  // of the operand
+    const float* row;  // of out's rows (may be null)
+    __device__ __forceinline__ float both() const { return inverse_power(scale_for(*top)) * (1.f / kG); }
 };
 
 // out[n][m] (rows of ld) = what A[m] B[n] add up to over the steps, unscaled, as OUT; or, with `part`, as it is to part[z] (+ what lies
-// there), a share of the steps each.
-template <typename C, typename OUT>
-__global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, NtOperand bn, int tiles_m, int tiles_n, int steps, int shares,
-                                                                  OUT* out, int64_t ld, float* part, int add, Unscale by)
+// there), a share of the steps each.  KB: B lies across k, and n counts its columns.
+template <typename C, bool KB, typename OUT>
+__global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, NtOperand bn, int64_t rows, int tiles_m, int tiles_n, int steps,
+                                                                  int shares, OUT* out, int64_t ld, float* part, int add, Unscale by)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int tm, tn;
@@ -468,16 +432,16 @@ __global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, 
     if (!nt_place((int)blockIdx.x - share * tiles8, tiles_m, tiles_n, tm, tn)) return;
     const int each = (steps + shares - 1) / shares, first = share * each, count = steps - first < each ? steps - first : each;
     f32x4 acc[C::TI][C::TJ];
-    nt_product<C>(am, (int64_t)tm * C::BM, bn, (int64_t)tn * C::BN, first, count, lds, acc);
+    nt_product<C, false, false, KB>(am, (int64_t)tm * C::BM, bn, (int64_t)tn * C::BN, first, count, lds, acc);
     const int lane = threadIdx.x & 63;
     const int64_t m0 = (int64_t)tm * C::BM + C::row0() + 4 * (lane >> 4), n0 = (int64_t)tn * C::BN + C::col0() + (lane & 15);
     const bool whole = (ld & 3) == 0;
-    const f32x2 f = part ? f32x2{1.f, 1.f} : by.factors();
-    float* sum = part ? part + (int64_t)share * bn.rows * ld : nullptr;
+    const float f = part ? 1.f : by.both();
+    float* sum = part ? part + (int64_t)share * rows * ld : nullptr;
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j) {
         const int64_t n = n0 + 16 * j;
-        if (n >= bn.rows) continue;
+        if (n >= rows) continue;
         const float row = !part && by.row ? by.row[n] : 1.f;
 #pragma unroll
         for (int i = 0; i < C::TI; ++i) {
@@ -485,7 +449,7 @@ __global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, 
             if (m >= am.rows) continue;
             f32x4 v = acc[i][j];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = v[e] * f[0] * f[1] * row;
+            for (int e = 0; e < 4; ++e) v[e] = v[e] * f * row;
             const int64_t at = n * ld + m;
             if (whole) {
                 if (sum) *reinterpret_cast<f32x4*>(sum + at) = add ? v + *reinterpret_cast<const f32x4*>(sum + at) : v;
@@ -509,11 +473,11 @@ __global__ __launch_bounds__(256) void xent_shares_kernel(const float* __restric
                                                           Unscale by)
 {
     const int64_t size = rows * ld;
-    const f32x2 f = by.factors();
+    const float f = by.both();
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
         float s = part[i];
         for (int k = 1; k < shares; ++k) s += part[k * size + i];
-        Elem<OUT>::store(out + i, s * f[0] * f[1] * (by.row ? by.row[i / ld] : 1.f));
+        Elem<OUT>::store(out + i, s * f * (by.row ? by.row[i / ld] : 1.f));
     }
 }
 
@@ -661,15 +625,15 @@ Cut cut_for(int64_t m, int64_t n, int steps, bool planes, int pieces_before)
     return best;
 }
 
-constexpr size_t kPieceBytes = (size_t)1 << 30;  // G of a piece of the vocabulary, both ways round, where the workspace has room for it
+constexpr size_t kPieceBytes = (size_t)1 << 29;  // G of a piece of the vocabulary, where the workspace has room for it
 
 struct BwdArea {
     Sides sides;
-    uint16_t *wt, *xt, *g, *gt;
-    float *dl, *top, *tops, *dx_part, *dw_part;  // top: largest dl, x, W; tops: of workgroups, x then W
+    uint16_t *wt, *xt, *g;
+    float *dl, *top, *tops, *dx_part, *dw_part;  // top: largest of x (times dl) and W; tops: of workgroups, x then W
     int piece;                                   // entries of the vocabulary, whole tiles
     Cut dx_cut, dw_cut, dw_last;                 // of a whole piece, and of the last one
-    uint32_t g_half, gt_half, wt_half, xt_half;
+    uint32_t g_half, wt_half, xt_half;
     int entries_of(const Plan& p, int v0) const { return p.vocab - v0 < piece ? p.vocab - v0 : piece; }
     size_t lay(const Plan& p, char* base, int64_t tiles_of_piece)
     {
@@ -683,15 +647,13 @@ struct BwdArea {
         dw_cut = cut_for(p.width, first, (int)((p.rows + per - 1) / per), p.f32, 0);
         dw_last = cut_for(p.width, last, (int)((p.rows + per - 1) / per), p.f32, 0);
         g_half = p.half(piece);
-        gt_half = p.half(tokens);
         wt_half = p.half((int64_t)p.parts() * p.bv());
         xt_half = p.half(tokens);
         wt = a.take<uint16_t>((size_t)p.width * wt_half);
         xt = a.take<uint16_t>((size_t)p.width * xt_half);
         g = a.take<uint16_t>((size_t)tokens * g_half);
-        gt = a.take<uint16_t>((size_t)piece * gt_half);
         dl = a.take<float>(p.rows);
-        top = a.take<float>(3);
+        top = a.take<float>(2);
         tops = a.take<float>(2 * kTops);
         dx_part = dx_cut.shares > 1 || several ? a.take<float>((size_t)dx_cut.shares * p.rows * p.width) : nullptr;
         const size_t one = dw_cut.shares > 1 ? (size_t)dw_cut.shares * first : 0, two = dw_last.shares > 1 ? (size_t)dw_last.shares * last : 0;
@@ -703,7 +665,7 @@ struct BwdArea {
     size_t fit(const Plan& p, char* base, size_t room)
     {
         const int64_t tiles = p.parts(), tokens = p.row_tiles() * p.bt(), across = (p.width + 255) / 256, round = 256 / across * (256 / p.bv());
-        int64_t most = (int64_t)(kPieceBytes / ((size_t)tokens * (p.f32 ? 8 : 4))) / p.bv();
+        int64_t most = (int64_t)(kPieceBytes / ((size_t)tokens * (p.f32 ? 4 : 2))) / p.bv();
         most = most < 1 ? 1 : most > tiles ? tiles : most;
         for (; most > 0; most = most > 16 ? most - most / 8 : most - 1) {
             const int64_t each = most < tiles && round > 0 && most >= round ? most / round * round : most;
@@ -768,17 +730,18 @@ int run_part(const Logits& l, f32x2* part, int parts, float* hit, hipStream_t st
     return launched();
 }
 template <typename C, bool TAIL>
-int run_grad(const Logits& l, const float* lse, const BwdArea& a, uint16_t* g, uint16_t* gt, hipStream_t st)
+int run_grad(const Logits& l, const float* lse, const BwdArea& a, hipStream_t st)
 {
     if constexpr (!TAIL && C::KIND != kF16x2)
-        if (l.tail < 8) return run_grad<C, true>(l, lse, a, g, gt, st);
+        if (l.tail < 8) return run_grad<C, true>(l, lse, a, st);
     if (allow_dynamic_lds((const void*)xent_grad_kernel<C, TAIL>, C::LDS_BYTES) != hipSuccess) return -4;
-    xent_grad_kernel<C, TAIL><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, lse, a.dl, a.top, g, a.g_half, gt, a.gt_half);
+    xent_grad_kernel<C, TAIL><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, lse, a.dl, a.g, a.g_half);
     return launched();
 }
 
-struct Job {  // out (b.rows x a.rows, rows of ld) from operands a and b
+struct Job {  // out (rows x a.rows, rows of ld) from operands a and b
     NtOperand a, b;
+    int64_t rows;
     int steps;
     void* out;
     int64_t ld;
@@ -786,22 +749,22 @@ struct Job {  // out (b.rows x a.rows, rows of ld) from operands a and b
     bool add, last;
     Unscale by;
 };
-template <typename C, typename OUT>
+template <typename C, bool KB, typename OUT>
 int run_product(const Job& j, int shares, hipStream_t st)
 {
-    if (allow_dynamic_lds((const void*)xent_product_kernel<C, OUT>, C::LDS_BYTES) != hipSuccess) return -4;
-    const int tm = (int)((j.a.rows + C::BM - 1) / C::BM), tn = (int)((j.b.rows + C::BN - 1) / C::BN);
-    xent_product_kernel<C, OUT><<<nt_grid(tm, tn) * shares, C::THREADS, C::LDS_BYTES, st>>>(j.a, j.b, tm, tn, j.steps, shares, (OUT*)j.out, j.ld,
-                                                                                            j.part, j.add, j.by);
+    if (allow_dynamic_lds((const void*)xent_product_kernel<C, KB, OUT>, C::LDS_BYTES) != hipSuccess) return -4;
+    const int tm = (int)((j.a.rows + C::BM - 1) / C::BM), tn = (int)((j.rows + C::BN - 1) / C::BN);
+    xent_product_kernel<C, KB, OUT><<<nt_grid(tm, tn) * shares, C::THREADS, C::LDS_BYTES, st>>>(j.a, j.b, j.rows, tm, tn, j.steps, shares,
+                                                                                                (OUT*)j.out, j.ld, j.part, j.add, j.by);
     return launched();
 }
-template <typename B, typename M, typename OUT>
+template <typename B, typename M, bool KB, typename OUT>
 int product(const Job& j, const Cut& cut, hipStream_t st)
 {
-    if (int rc = cut.big ? run_product<B, OUT>(j, cut.shares, st) : run_product<M, OUT>(j, cut.shares, st)) return rc;
+    if (int rc = cut.big ? run_product<B, KB, OUT>(j, cut.shares, st) : run_product<M, KB, OUT>(j, cut.shares, st)) return rc;
     if (!j.part || !j.last) return 0;
-    const int64_t size = j.b.rows * j.ld, groups = (size + 1023) / 1024;
-    xent_shares_kernel<OUT><<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(j.part, cut.shares, j.b.rows, j.ld, (OUT*)j.out, j.by);
+    const int64_t size = j.rows * j.ld, groups = (size + 1023) / 1024;
+    xent_shares_kernel<OUT><<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(j.part, cut.shares, j.rows, j.ld, (OUT*)j.out, j.by);
     return launched();
 }
 
@@ -852,7 +815,7 @@ int xent_bwd(const void* x, const void* w, const int64_t* target, const float* l
     const Plan p{dtype == 0, rows, vocab, width, false};
     BwdArea a;
     if (!a.fit(p, (char*)ws, ws_bytes)) return -3;
-    xent_upstream_kernel<<<1, 1024, 0, st>>>(dloss, dloss_stride, divisor, target, ignore, vocab, rows, a.dl, a.top);
+    xent_upstream_kernel<<<(unsigned)((rows + 255) / 256), 256, 0, st>>>(dloss, dloss_stride, divisor, target, ignore, vocab, rows, a.dl);
     if (int rc = launched()) return rc;
     if (int rc = pack_sides(p, a.sides, x, w, a.dl, a.tops, st)) return rc;
     const unsigned columns = (unsigned)((width + 63) / 64);
@@ -863,8 +826,8 @@ int xent_bwd(const void* x, const void* w, const int64_t* target, const float* l
         return launched();
     };
     int rc = 0;
-    if (dx && (rc = pack_columns(w, vocab, a.wt, a.wt_half, nullptr, a.tops + kTops, a.top + 2))) return rc;
-    if (dw && (rc = pack_columns(x, rows, a.xt, a.xt_half, a.dl, a.tops, a.top + 1))) return rc;
+    if (dx && (rc = pack_columns(w, vocab, a.wt, a.wt_half, nullptr, a.tops + kTops, a.top + 1))) return rc;
+    if (dw && (rc = pack_columns(x, rows, a.xt, a.xt_half, a.dl, a.tops, a.top))) return rc;
     Logits l = logits_of(p, a.sides, x, w, target);
     const int per = p.per_step();
     for (int v0 = 0; v0 < vocab; v0 += a.piece) {
@@ -872,28 +835,27 @@ int xent_bwd(const void* x, const void* w, const int64_t* target, const float* l
         const bool last = v0 + a.piece >= vocab;
         l.v0 = v0;
         l.tiles_v = (entries + p.bv() - 1) / p.bv();
-        uint16_t *g = dx ? a.g : nullptr, *gt = dw ? a.gt : nullptr;
-        if (p.f32) rc = by_tile<Big2, Mid2, Low2, Low2>(p, [&](auto c) { return run_grad<decltype(c), false>(l, lse, a, g, gt, st); });
-        else rc = by_tile<Big, Mid, Low, Low>(p, [&](auto c) { return run_grad<decltype(c), false>(l, lse, a, g, gt, st); });
+        if (p.f32) rc = by_tile<Big2, Mid2, Low2, Low2>(p, [&](auto c) { return run_grad<decltype(c), false>(l, lse, a, st); });
+        else rc = by_tile<Big, Mid, Low, Low>(p, [&](auto c) { return run_grad<decltype(c), false>(l, lse, a, st); });
         if (rc) return rc;
         if (dx) {
             // features inside, rows of x outside
-            Job j{{a.wt + (size_t)v0 / per * 64, width, a.wt_half * 2}, {a.g, rows, a.g_half * 2}, (entries + per - 1) / per, dx, width, a.dx_part, v0 > 0,
-                  last, {a.top + 2, nullptr, a.dl}};
-            rc = p.f32 ? product<Big2, Mid2, float>(j, a.dx_cut, st) : product<Big16, Mid16, uint16_t>(j, a.dx_cut, st);
+            Job j{{a.wt + (size_t)v0 / per * 64, width, a.wt_half * 2}, {a.g, rows, a.g_half * 2}, rows, (entries + per - 1) / per, dx, width,
+                  a.dx_part, v0 > 0, last, {a.top + 1, a.dl}};
+            rc = p.f32 ? product<Big2, Mid2, false, float>(j, a.dx_cut, st) : product<Big16, Mid16, false, uint16_t>(j, a.dx_cut, st);
             if (rc) return rc;
         }
         if (dw) {
             const Cut& cut = last ? a.dw_last : a.dw_cut;
-            Job j{{a.xt, width, a.xt_half * 2}, {a.gt, entries, a.gt_half * 2}, (int)((rows + per - 1) / per), nullptr, width,
-                  cut.shares > 1 ? a.dw_part : nullptr, false, true, {a.top + 1, a.top, nullptr}};
+            Job j{{a.xt, width, a.xt_half * 2}, {a.g, rows, a.g_half * 2}, entries, (int)((rows + per - 1) / per), nullptr, width,
+                  cut.shares > 1 ? a.dw_part : nullptr, false, true, {a.top, nullptr}};
             const size_t at = (size_t)v0 * width;
             if (dw_f32) {
                 j.out = (float*)dw + at;
-                rc = p.f32 ? product<Big2, Mid2, float>(j, cut, st) : product<Big16, Mid16, float>(j, cut, st);
+                rc = p.f32 ? product<Big2, Mid2, true, float>(j, cut, st) : product<Big16, Mid16, true, float>(j, cut, st);
             } else {
                 j.out = (uint16_t*)dw + at;
-                rc = product<Big16, Mid16, uint16_t>(j, cut, st);
+                rc = product<Big16, Mid16, true, uint16_t>(j, cut, st);
             }
             if (rc) return rc;
         }

@@ -95,20 +95,22 @@ def test_a_short_workspace_takes_the_vocabulary_in_pieces(ops, dtype):
     g = torch.ones(())
     want = Exact(x, W, target, torch.ones(rows), dtype)
     need = binding.monarch_xent_bwd_workspace_bytes(rows, vocab, width, code)
-    seen = set()
-    for bytes_ in (need, need - (1 << 20), need - (2 << 20)):
-        ws = torch.empty(bytes_, dtype=torch.uint8, device="cuda")
+
+    def serves(bytes_):
         try:
-            _, _, dx, dW = run(binding, x, W, target, g, workspace=ws)
+            return run(binding, x, W, target, g, workspace=torch.empty(bytes_, dtype=torch.uint8, device="cuda"))
         except binding.MonarchError as e:
-            assert e.args and "workspace" in str(e)
-            continue
-        seen.add(bytes_)
+            assert "workspace" in str(e)
+            return None
+    refused, least = 0, need      # the shortest that serves
+    while least - refused > 256:
+        middle = (refused + least) // 2
+        refused, least = (refused, middle) if serves(middle) else (middle, least)
+    assert least < need
+    for bytes_ in (need, (need + least) // 2, least):
+        _, _, dx, dW = serves(bytes_)
         within(dx, want.dx, want.dx_bound, "dx")
         within(dW, want.dW, want.dW_bound, "dW")
-    assert len(seen) >= 2, (need, seen)
-    with pytest.raises(binding.MonarchError):
-        run(binding, x, W, target, g, workspace=torch.empty(1 << 16, dtype=torch.uint8, device="cuda"))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -24,14 +24,15 @@ struct NtOperand {
 enum NtKind { kBf16, kF16, kF16x2, kF32 };
 
 // A workgroup's BM x BN tile, a wave's WM x WN part of it.
-template <int BM_, int BN_, int WM_, int WN_, NtKind KIND_, int RING_ = 2>
+template <int BM_, int BN_, int WM_, int WN_, NtKind KIND_, int RING_ = 2, int SUB_ = 1>
 struct NtTile {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, RING = RING_;  // RING: steps in LDS
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, RING = RING_;
+    static constexpr int SUB = SUB_;  // steps that come together, between two barriers; RING times as many are in LDS
     static constexpr NtKind KIND = KIND_;
     static constexpr int PL = KIND == kF16x2 ? 2 : 1;  // planes
     static constexpr int WAVES = (BM / WM) * (BN / WN), THREADS = 64 * WAVES;
     static constexpr int TI = WM / 16, TJ = WN / 16;
-    static constexpr int BUFFER = (BM + BN) * 128, LDS_BYTES = RING * BUFFER;
+    static constexpr int BUFFER = SUB * (BM + BN) * 128, LDS_BYTES = RING * BUFFER;
     static constexpr int ASK_A = BM / 8 / WAVES, ASK_B = BN / 8 / WAVES;  // requests of a wave per step, 8 rows each
     static_assert(RING >= 2 && RING <= 4, "ring");
     static_assert(ASK_A * 8 * WAVES == BM && ASK_B * 8 * WAVES == BN, "whole requests");
@@ -42,33 +43,36 @@ struct NtTile {
 
 __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// c += what a step's two halves of the operands contribute
-template <NtKind KIND>
-__device__ __forceinline__ f32x4 nt_step(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1, f32x4 c)
+// c[j] += what a step's two halves of a and b[.][j] contribute; one product of every c before the next, since each waits for the one before it
+template <NtKind KIND, int TJ>
+__device__ __forceinline__ void nt_step(u32x4 a0, u32x4 a1, const u32x4 (&b)[2][TJ], f32x4 (&c)[TJ])
 {
-    if constexpr (KIND == kBf16) {
-        c = mfma16(as_bf16x8(a0), as_bf16x8(b0), c);
-        return mfma16(as_bf16x8(a1), as_bf16x8(b1), c);
-    } else if constexpr (KIND == kF32) {
+    if constexpr (KIND == kF32) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a0[e]), __uint_as_float(b0[e]), c, 0, 0, 0);
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a1[e]), __uint_as_float(b1[e]), c, 0, 0, 0);
-        return c;
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < TJ; ++j)
+                    c[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(h ? a1[e] : a0[e]), __uint_as_float(b[h][j][e]), c[j], 0, 0, 0);
     } else {
-        const f16x8 p0 = __builtin_bit_cast(f16x8, a0), p1 = __builtin_bit_cast(f16x8, a1), q0 = __builtin_bit_cast(f16x8, b0), q1 = __builtin_bit_cast(f16x8, b1);
-        c = mfma16(p0, q0, c);
-        if constexpr (KIND == kF16) return mfma16(p1, q1, c);
-        c = mfma16(p0, q1, c);
-        return mfma16(p1, q0, c);
+        constexpr int PRODUCTS = KIND == kF16x2 ? 3 : 2;  // two planes: upper x upper, upper x lower, lower x upper
+#pragma unroll
+        for (int t = 0; t < PRODUCTS; ++t)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+                const u32x4 p = t == PRODUCTS - 1 ? a1 : a0, q = KIND == kF16x2 ? b[t & 1][j] : b[t][j];
+                if constexpr (KIND == kBf16) c[j] = mfma16(as_bf16x8(p), as_bf16x8(q), c[j]);
+                else c[j] = mfma16(__builtin_bit_cast(f16x8, p), __builtin_bit_cast(f16x8, q), c[j]);
+            }
     }
 }
 
 #ifdef __HIP_DEVICE_COMPILE__  // (buffer descriptors are no type of the host's)
-// `rows` rows (less where the operand ends) from `row`, `skip` bytes into it
-__device__ __forceinline__ auto nt_rsrc(const NtOperand& o, int64_t row, int rows_of_tile, uint32_t skip)
+// `rows_of_tile` rows (fewer where the operand ends, none unless live) from `row`, `skip` bytes into it; what is not there reads as zeros
+__device__ __forceinline__ auto nt_rsrc(const NtOperand& o, int64_t row, int rows_of_tile, uint32_t skip, bool live)
 {
-    int64_t rows = o.rows - row;
+    int64_t rows = live ? o.rows - row : 0;
     rows = rows < 0 ? 0 : rows > rows_of_tile ? rows_of_tile : rows;
     const uint32_t bytes = (uint32_t)rows * o.row_bytes;
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((const char*)o.base) + row * (int64_t)o.row_bytes + skip, 0,
@@ -82,7 +86,9 @@ __device__ __forceinline__ auto nt_rsrc(const NtOperand& o, int64_t row, int row
 template <typename C, int SIDE, int ASKS, bool ACROSS>
 struct NtSide {
     static constexpr int ROW = ACROSS ? SIDE * 2 * C::PL : 128, K_ROWS = 64 / C::PL;
-    static_assert(!ACROSS || ROW >= 256, "pieces for eight keys");
+    static_assert(!ACROSS || ROW >= 128, "pieces for four keys");
+    // (in rows of 128 bytes the neighbours lie in different halves of the banks)
+    static __device__ __forceinline__ uint32_t key(uint32_t row) { return ROW == 128 ? (row >> 1 & 1) | (row >> 3 & 1) << 1 : (row & 3) | (row >> 3 & 1) << 2; }
     const NtOperand& o;
     int64_t first;  // row (column) of the tile
     uint32_t at[ASKS];
@@ -92,17 +98,17 @@ struct NtSide {
 #pragma unroll
         for (int i = 0; i < ASKS; ++i) {
             if constexpr (ACROSS) {
-                const uint32_t p = (wave + i * C::WAVES) * 1024 + lane * 16, row = p / ROW, in = p % ROW, key = (row & 3) | (row >> 3 & 1) << 2;
-                at[i] = row * o.row_bytes + (in ^ key << 5);
+                const uint32_t p = (wave + i * C::WAVES) * 1024 + lane * 16, row = p / ROW, in = p % ROW;
+                at[i] = row * o.row_bytes + (in ^ key(row) << 5);
             } else {
                 at[i] = ((wave + i * C::WAVES) * 8 + (lane >> 3)) * o.row_bytes + 16 * ((lane & 7) ^ (lane >> 3));
             }
         }
     }
     template <typename P>
-    __device__ __forceinline__ void ask(int step, P to) const  // to: of the wave's first request
+    __device__ __forceinline__ void ask(int step, bool live, P to) const  // to: of the wave's first request
     {
-        const auto r = ACROSS ? nt_rsrc(o, (int64_t)step * K_ROWS, K_ROWS, (uint32_t)(first * 2 * C::PL)) : nt_rsrc(o, first, SIDE, 0);
+        const auto r = ACROSS ? nt_rsrc(o, (int64_t)step * K_ROWS, K_ROWS, (uint32_t)(first * 2 * C::PL), live) : nt_rsrc(o, first, SIDE, 0, live);
 #pragma unroll
         for (int i = 0; i < ASKS; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(to + i * C::WAVES * 1024), 16, at[i],
@@ -132,7 +138,7 @@ __device__ __forceinline__ u32x4 nt_whole(const Frag& f) { return u32x4{f.lo[0],
 #endif
 
 // acc[i][j][e] = D[a0 + row0() + 16 i + 4 (lane / 16) + e][b0 + col0() + 16 j + lane % 16] over `steps` steps from `step0`.
-// The next RING - 1 steps come straight into LDS while a step's products run; one barrier a step.  KA, KB: A, B lie across k.  TAIL (both along k): only
+// The next steps come straight into LDS while this one's products run.  KA, KB: A, B lie across k.  TAIL (both along k): only
 // the first `tail` of the eight 16-byte pieces of the last step count (the rows end there, and what follows is not theirs).
 template <typename C, bool TAIL = false, bool KA = false, bool KB = false>
 __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const NtOperand& B, int64_t b0, int step0, int steps,
@@ -149,19 +155,25 @@ __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const
     const SideA side_a(A, a0, wave, lane);
     const SideB side_b(B, b0, wave, lane);
     auto to = (__attribute__((address_space(3))) unsigned char*)lds + wave * 1024;
-    auto ask = [&](int step, int buffer) {
-        side_a.ask(step, to + buffer * C::BUFFER);
-        side_b.ask(step, to + buffer * C::BUFFER + C::BM * 128);
+    const int groups = (steps + C::SUB - 1) / C::SUB;
+    auto ask = [&](int group, int buffer) {
+#pragma unroll
+        for (int u = 0; u < C::SUB; ++u) {
+            const int step = group * C::SUB + u;
+            const bool live = C::SUB == 1 || step < steps;  // (past the end: zeros)
+            side_a.ask(step0 + step, live, to + buffer * C::BUFFER + u * (C::BM + C::BN) * 128);
+            side_b.ask(step0 + step, live, to + buffer * C::BUFFER + (u * (C::BM + C::BN) + C::BM) * 128);
+        }
     };
     const int r16 = lane & 15, at0 = 16 * ((lane >> 4) ^ (lane & 7)), at1 = at0 ^ 64;
     const unsigned char* fa = lds + (C::row0() + r16) * 128;
     const unsigned char* fb = lds + C::BM * 128 + (C::col0() + r16) * 128;
     // across k: the lane's row among 8g .. 8g+3, its key, its four columns
-    const uint32_t row_k = 8 * (lane >> 4) + (r16 >> 2), in_k = ((row_k & 3) | (row_k >> 3 & 1) << 2) << 5 | 8 * (lane & 3);
+    const uint32_t row_k = 8 * (lane >> 4) + (r16 >> 2), in_k = 8 * (lane & 3);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
-    const uint32_t ka = lds0 + row_k * SideA::ROW + in_k, kb = lds0 + C::BM * 128 + row_k * SideB::ROW + in_k;
-    auto products = [&](auto cut, int buffer) {
-        const unsigned char *pa = fa + buffer * C::BUFFER, *pb = fb + buffer * C::BUFFER;
+    const uint32_t ka = lds0 + (row_k * SideA::ROW | SideA::key(row_k) << 5 | in_k), kb = lds0 + C::BM * 128 + (row_k * SideB::ROW | SideB::key(row_k) << 5 | in_k);
+    auto products = [&](auto cut, int offset) {  // of the step that lies there
+        const unsigned char *pa = fa + offset, *pb = fb + offset;
         const bool in0 = lane >> 4 < tail, in1 = 4 + (lane >> 4) < tail;
         auto half = [&](const unsigned char* p, bool in) {
             u32x4 v = lds128(p);
@@ -177,14 +189,18 @@ __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const
                 b[1][j] = half(pb + j * 2048 + at1, in1);
             }
         }
-        Frag a[2][2], bk[KB ? C::TJ : 1][2];
+        // fragments of A under way: one ahead, or (few of them) all
+        constexpr int AHEAD = C::TI <= 2 ? C::TI : 1;
+        Frag a[AHEAD + 1][2], bk[KB ? C::TJ : 1][2];
         if constexpr (KB) {
 #pragma unroll
-            for (int j = 0; j < C::TJ; ++j) nt_read_across<C, SideB::ROW>(kb + buffer * C::BUFFER, C::col0() + 16 * j, bk[j]);
+            for (int j = 0; j < C::TJ; ++j) nt_read_across<C, SideB::ROW>(kb + offset, C::col0() + 16 * j, bk[j]);
         }
         if constexpr (KA) {
-            nt_read_across<C, SideA::ROW>(ka + buffer * C::BUFFER, C::row0(), a[0]);
-            lgkm_wait(a[0]);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) nt_read_across<C, SideA::ROW>(ka + offset, C::row0() + 16 * i, a[i]);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) lgkm_wait(a[i]);
         }
         if constexpr (KB) {
 #pragma unroll
@@ -197,35 +213,42 @@ __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const
         if constexpr (KA) {
 #pragma unroll
             for (int i = 0; i < C::TI; ++i) {
+                const int now = i % (AHEAD + 1), next = (i + AHEAD) % (AHEAD + 1);
                 // (the next fragment travels during this one's products)
-                if (i + 1 < C::TI) nt_read_across<C, SideA::ROW>(ka + buffer * C::BUFFER, C::row0() + 16 * (i + 1), a[(i + 1) & 1]);
-#pragma unroll
-                for (int j = 0; j < C::TJ; ++j)
-                    acc[i][j] = nt_step<C::KIND>(nt_whole(a[i & 1][0]), nt_whole(a[i & 1][1]), b[0][j], b[1][j], acc[i][j]);
-                if (i + 1 < C::TI) lgkm_wait(a[(i + 1) & 1]);
+                if (i + AHEAD < C::TI) nt_read_across<C, SideA::ROW>(ka + offset, C::row0() + 16 * (i + AHEAD), a[next]);
+                nt_step<C::KIND>(nt_whole(a[now][0]), nt_whole(a[now][1]), b, acc[i]);
+                if (i + AHEAD < C::TI) lgkm_wait(a[next]);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < C::TI; ++i) {
                 const u32x4 u = half(pa + i * 2048 + at0, in0), v = half(pa + i * 2048 + at1, in1);
-#pragma unroll
-                for (int j = 0; j < C::TJ; ++j) acc[i][j] = nt_step<C::KIND>(u, v, b[0][j], b[1][j], acc[i][j]);
+                nt_step<C::KIND>(u, v, b, acc[i]);
             }
         }
     };
-    constexpr int PENDING = C::ASK_A + C::ASK_B;
-    for (int s = 0; s < C::RING - 1 && s < steps; ++s) ask(step0 + s, s);
+    constexpr int PENDING = C::SUB * (C::ASK_A + C::ASK_B);
+    for (int s = 0; s < C::RING - 1 && s < groups; ++s) ask(s, s);
     int buffer = 0;
-    for (int s = 0; s < steps; ++s) {
-        // step s has landed once only what was asked for after it is outstanding
-        if (C::RING == 4 && s + 2 < steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * PENDING) : "memory");
-        else if (C::RING >= 3 && s + 1 < steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PENDING) : "memory");
+    for (int s = 0; s < groups; ++s) {
+        // group s has landed once only what was asked for after it is outstanding
+        if (C::RING == 4 && s + 2 < groups) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * PENDING) : "memory");
+        else if (C::RING >= 3 && s + 1 < groups) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PENDING) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();  // ... for every wave, and nobody reads step s - 1 any more
+        __builtin_amdgcn_s_barrier();  // ... for every wave, and nobody reads group s - 1 any more
         asm volatile("" ::: "memory");
-        if (s + C::RING - 1 < steps) ask(step0 + s + C::RING - 1, buffer ? buffer - 1 : C::RING - 1);
-        if (TAIL && s + 1 == steps && tail < 8) products(std::true_type{}, buffer);
-        else products(std::false_type{}, buffer);
+        if (s + C::RING - 1 < groups) ask(s + C::RING - 1, buffer ? buffer - 1 : C::RING - 1);
+#pragma unroll
+        for (int u = 0; u < C::SUB; ++u) {
+            const int step = s * C::SUB + u, offset = buffer * C::BUFFER + u * (C::BM + C::BN) * 128;
+            if constexpr (TAIL) {
+                if (step + 1 == steps && tail < 8) {
+                    products(std::true_type{}, offset);
+                    continue;
+                }
+            }
+            products(std::false_type{}, offset);
+        }
         buffer = buffer + 1 == C::RING ? 0 : buffer + 1;
     }
 #endif

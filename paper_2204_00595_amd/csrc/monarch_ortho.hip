@@ -103,6 +103,38 @@ __global__ __launch_bounds__(256) void ortho_pack_kernel(Source s, const double*
     const int64_t size = (int64_t)s.m * s.n, at = (int64_t)(block - tensor * s.blocks) * size;
     const T* g = (const T*)s.g[tensor] + at;
     const float* v = MUON ? s.v[tensor] + at : nullptr;
+    const int i0 = blockIdx.x * 64, j0 = blockIdx.y * 64;
+    float u[16];  // (on their way while the norm is made)
+    if ((s.n & 3) == 0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + 16 * k + (tid >> 4), j = j0 + (tid & 15) * 4;
+            f32x4 w = {0.f, 0.f, 0.f, 0.f};
+            if (i < s.m && j < s.n) {
+                const int64_t p = (int64_t)i * s.n + j;
+                w = load4(g + p);
+                if constexpr (MUON) {
+                    const f32x4 vi = load4(v + p);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = s.nesterov ? fmaf(s.momentum, vi[e], w[e]) : vi[e];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[4 * k + e] = w[e];
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int i = i0 + 16 * (k >> 2) + (tid >> 4), j = j0 + (tid & 15) * 4 + (k & 3);
+            u[k] = 0.f;
+            if (i < s.m && j < s.n) {
+                const int64_t p = (int64_t)i * s.n + j;
+                const float gi = Elem<T>::load(g + p);
+                u[k] = gi;
+                if constexpr (MUON) u[k] = s.nesterov ? fmaf(s.momentum, v[p], gi) : v[p];
+            }
+        }
+    }
     double sum = 0;
     for (int i = tid; i < parts; i += 256) sum += part[(int64_t)block * parts + i];
 #pragma unroll
@@ -110,20 +142,8 @@ __global__ __launch_bounds__(256) void ortho_pack_kernel(Source s, const double*
     if ((tid & 63) == 0) wave[tid >> 6] = sum;
     __syncthreads();
     const double by = (double)kX / (sqrt(wave[0] + wave[1] + wave[2] + wave[3]) + (double)eps);
-    const int i0 = blockIdx.x * 64, j0 = blockIdx.y * 64;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const int i = i0 + 4 * k + (tid >> 6), j = j0 + (tid & 63);
-        float u = 0.f;
-        if (i < s.m && j < s.n) {
-            const int64_t p = (int64_t)i * s.n + j;
-            const float gi = Elem<T>::load(g + p);
-            u = gi;
-            if constexpr (MUON) u = s.nesterov ? fmaf(s.momentum, v[p], gi) : v[p];
-            u = (float)(u * by);
-        }
-        tile[4 * k + (tid >> 6)][tid & 63] = u;
-    }
+    for (int k = 0; k < 16; ++k) tile[16 * (k >> 2) + (tid >> 4)][(tid & 15) * 4 + (k & 3)] = (float)(u[k] * by);
     __syncthreads();
     const int row0 = TURN ? j0 : i0, col0 = TURN ? i0 : j0, rows = TURN ? s.n : s.m;
     const uint32_t half = row_half(TURN ? s.m : s.n);
@@ -132,10 +152,10 @@ __global__ __launch_bounds__(256) void ortho_pack_kernel(Source s, const double*
     for (int k = 0; k < 4; ++k) {
         const int piece = 256 * k + tid, r = piece >> 4, c = (piece & 15) * 4;
         if (row0 + r >= rows || (uint32_t)(col0 + c) * 2 >= half) continue;
-        f32x4 u;
+        f32x4 w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) u[e] = TURN ? tile[c + e][r] : tile[r][c + e];
-        const TwoPlanes h = split_planes(u);
+        for (int e = 0; e < 4; ++e) w[e] = TURN ? tile[c + e][r] : tile[r][c + e];
+        const TwoPlanes h = split_planes(w);
 #pragma unroll
         for (int plane = 0; plane < 2; ++plane) *reinterpret_cast<u32x2*>(to + (int64_t)(row0 + r) * half + place(col0 + c, plane)) = h.p[plane];
     }
@@ -199,6 +219,22 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
         tb = in / p.tiles_a;
         ta = in - tb * p.tiles_a;
     }
+    const int lane = threadIdx.x & 63;
+    const int m0 = ta * C::BM + C::row0() + 4 * (lane >> 4), n0 = tb * C::BN + C::col0() + (lane & 15);
+    u32x2 gram[PART == kPoly ? C::TI : 1][PART == kPoly ? C::TJ : 1][2];  // (on its way during the products)
+    if constexpr (PART == kPoly) {
+#pragma unroll
+        for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TJ; ++j)
+#pragma unroll
+                for (int plane = 0; plane < 2; ++plane) {
+                    const int m = m0 + 16 * i, n = n0 + 16 * j;
+                    gram[i][j][plane] = u32x2{0, 0};
+                    if (n < p.b_rows && (uint32_t)m * 2 < p.rows_half)
+                        gram[i][j][plane] = *reinterpret_cast<const u32x2*>(p.gram + ((int64_t)block * p.b_rows + n) * p.rows_half + place(m, plane));
+                }
+    }
     f32x4 acc[C::TI][C::TJ];
     if constexpr (PART == kGram) {
         const NtOperand x{p.a + (int64_t)block * p.k_rows * p.half, p.k_rows, p.half * 2};
@@ -208,8 +244,6 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
         const NtOperand b{p.b + (int64_t)block * p.b_rows * p.half, p.b_rows, p.half * 2};
         nt_product<C>(a, (int64_t)ta * C::BM, b, (int64_t)tb * C::BN, 0, (int)(p.half / 64), lds, acc);
     }
-    const int lane = threadIdx.x & 63;
-    const int m0 = ta * C::BM + C::row0() + 4 * (lane >> 4), n0 = tb * C::BN + C::col0() + (lane & 15);
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j)
 #pragma unroll
@@ -237,17 +271,12 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
                 if constexpr (PART == kNext) v *= 1.f / kP;
                 if constexpr (PART == kPoly) {
                     v *= p.cc * (kP / (kA * kA));
-                    if (in_rows) {
-                        const uint16_t* g = p.gram + ((int64_t)block * p.b_rows + n) * p.rows_half;
 #pragma unroll
-                        for (int plane = 0; plane < 2; ++plane) {
-                            const u32x2 u = *reinterpret_cast<const u32x2*>(g + place(m, plane));
+                    for (int e = 0; e < 4; ++e) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) v[e] = fmaf(p.cb * (kP / kA), f16_value(u[e >> 1] >> (16 * (e & 1))), v[e]);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (m + e == n) v[e] = fmaf(p.ca, kP, v[e]);
+                        for (int plane = 0; plane < 2; ++plane)
+                            v[e] = fmaf(p.cb * (kP / kA), f16_value(gram[i][j][plane][e >> 1] >> (16 * (e & 1))), v[e]);
+                        if (m + e == n && n < p.b_rows) v[e] = fmaf(p.ca, kP, v[e]);
                     }
                 }
                 if constexpr (PART == kGram) {  // (across, the numbers past a row's last are the next row's)
@@ -296,17 +325,16 @@ __device__ __forceinline__ void small_product(const unsigned char* a, const unsi
         for (int j = 0; j < K::T; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < K::STEPS; ++s) {
-        u32x4 b0[K::T], b1[K::T];
+        u32x4 q[2][K::T];
 #pragma unroll
         for (int j = 0; j < K::T; ++j) {
-            b0[j] = lds128(pb + s * S * 128 + j * 2048 + at0);
-            b1[j] = lds128(pb + s * S * 128 + j * 2048 + at1);
+            q[0][j] = lds128(pb + s * S * 128 + j * 2048 + at0);
+            q[1][j] = lds128(pb + s * S * 128 + j * 2048 + at1);
         }
 #pragma unroll
         for (int i = 0; i < K::T; ++i) {
             const u32x4 a0 = lds128(pa + s * S * 128 + i * 2048 + at0), a1 = lds128(pa + s * S * 128 + i * 2048 + at1);
-#pragma unroll
-            for (int j = 0; j < K::T; ++j) acc[i][j] = nt_step<kF16x2>(a0, a1, b0[j], b1[j], acc[i][j]);
+            nt_step<kF16x2>(a0, a1, q, acc[i]);
         }
     }
 }
@@ -466,11 +494,16 @@ int run_product(Product p, const Sink& sink, hipStream_t st)
 template <Part PART, typename T, Out OUT>
 int product(const Product& p, const Sink& sink, hipStream_t st)
 {
-    using Low = NtTile<64, 64, 32, 32, kF16x2>;
-    using Mid = NtTile<128, 128, 64, 64, kF16x2>;
-    const int64_t a = (p.a_rows + 127) / 128, b = (p.b_rows + 127) / 128;
-    const int64_t mid = (PART == kGram || PART == kPoly ? a * (a + 1) / 2 : a * b) * p.blocks;
-    return mid >= 256 ? run_product<Mid, PART, T, OUT>(p, sink, st) : run_product<Low, PART, T, OUT>(p, sink, st);
+    using Big = NtTile<128, 128, 64, 64, kF16x2>;
+    using Mid = NtTile<64, 64, 32, 32, kF16x2, 2, 2>;
+    using Low = NtTile<32, 32, 16, 16, kF16x2, 2, 2>;
+    const auto tiles = [&](int side) {
+        const int64_t a = (p.a_rows + side - 1) / side, b = (p.b_rows + side - 1) / side;
+        return (PART == kGram || PART == kPoly ? a * (a + 1) / 2 : a * b) * p.blocks;
+    };
+    if (tiles(128) >= 256) return run_product<Big, PART, T, OUT>(p, sink, st);
+    if (tiles(64) >= 256) return run_product<Mid, PART, T, OUT>(p, sink, st);
+    return run_product<Low, PART, T, OUT>(p, sink, st);
 }
 
 template <typename T, Out OUT>

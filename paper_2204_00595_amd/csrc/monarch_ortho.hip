@@ -244,31 +244,29 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
         const NtOperand b{p.b + (int64_t)block * p.b_rows * p.half, p.b_rows, p.half * 2};
         nt_product<C>(a, (int64_t)ta * C::BM, b, (int64_t)tb * C::BN, 0, (int)(p.half / 64), lds, acc);
     }
+    // Results leave by way of LDS, as whole lines: a lane holds four numbers of a row and its neighbours other rows', and written so a line comes in
+    // four pieces (P of 48 blocks of 256: 19 us, 6 without its stores).  A row there is two planes or fp32; piece u of row r in place u ^ (r % 16).
+    static_assert(C::BM == C::BN && C::BM * C::BM * 4 <= C::LDS_BYTES, "a tile of results takes the place of the operands");
+    constexpr int ROW = C::BM * 4, PIECES = ROW / 16, KEY = PIECES < 16 ? PIECES - 1 : 15;
+    const auto lds_at = [&](int r, int u) { return lds + r * ROW + 16 * (u ^ (r & KEY)); };
+    const int mw = C::row0() + 4 * (lane >> 4), nw = C::col0() + (lane & 15);  // m0, n0 in the tile
+    TwoPlanes h[C::TI][C::TJ];
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j)
 #pragma unroll
         for (int i = 0; i < C::TI; ++i) {
-            const int m = m0 + 16 * i, n = n0 + 16 * j;
             f32x4 v = acc[i][j];
+            const int r = nw + 16 * j, k = mw + 16 * i;
             if constexpr (PART == kLast) {
-                if (n >= p.b_rows || m >= p.a_rows) continue;
-                const int tensor = block / sink.blocks;
-                const int64_t at = (int64_t)(block - tensor * sink.blocks) * sink.m * sink.n + (int64_t)n * sink.n + m;
-                T* out = (T*)sink.out[tensor] + at;
-                float* master = OUT == kMasters ? sink.master[tensor] + at : nullptr;
-                v *= 1.f / (kX * kP);
-                if ((sink.n & 3) == 0) {
-                    put4<T, OUT>(sink, out, master, v);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (m + e < p.a_rows) put<T, OUT>(sink, out + e, OUT == kMasters ? master + e : nullptr, v[e]);
-                }
+                *reinterpret_cast<f32x4*>(lds_at(r, k >> 2)) = v * (1.f / (kX * kP));
             } else {
-                // (what lies past a row's numbers is zero: the rows that do not exist were read as zeros)
-                const bool in_rows = n < p.b_rows && (uint32_t)m * 2 < p.rows_half;
-                if constexpr (PART == kGram) v *= kA / (kX * kX);
+                // (what lies past a row's numbers is zero: the rows that do not exist were read as zeros; read across, they are the next row's)
                 if constexpr (PART == kNext) v *= 1.f / kP;
+                if constexpr (PART == kGram) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = m0 + 16 * i + e < p.a_rows && n0 + 16 * j < p.b_rows ? v[e] * (kA / (kX * kX)) : 0.f;
+                }
                 if constexpr (PART == kPoly) {
                     v *= p.cc * (kP / (kA * kA));
 #pragma unroll
@@ -276,27 +274,59 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
 #pragma unroll
                         for (int plane = 0; plane < 2; ++plane)
                             v[e] = fmaf(p.cb * (kP / kA), f16_value(gram[i][j][plane][e >> 1] >> (16 * (e & 1))), v[e]);
-                        if (m + e == n && n < p.b_rows) v[e] = fmaf(p.ca, kP, v[e]);
+                        if (m0 + 16 * i + e == n0 + 16 * j && n0 + 16 * j < p.b_rows) v[e] = fmaf(p.ca, kP, v[e]);
                     }
                 }
-                if constexpr (PART == kGram) {  // (across, the numbers past a row's last are the next row's)
+                h[i][j] = split_planes(v);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = m + e < p.a_rows ? v[e] : 0.f;
-                }
-                const TwoPlanes h = split_planes(v);
-#pragma unroll
-                for (int plane = 0; plane < 2; ++plane) {
-                    if (in_rows) *reinterpret_cast<u32x2*>(p.rows + ((int64_t)block * p.b_rows + n) * p.rows_half + place(m, plane)) = h.p[plane];
-                    if constexpr (HALF) {
-                        // the other side of the diagonal
-                        const u32x2 w = change_places(n < p.b_rows ? h.p[plane] : u32x2{0, 0});
-                        const int r = m + (lane & 3), c = n & ~3;
-                        if (ta != tb && r < p.a_rows && (uint32_t)c * 2 < p.rows_half)
-                            *reinterpret_cast<u32x2*>(p.rows + ((int64_t)block * p.a_rows + r) * p.rows_half + place(c, plane)) = w;
-                    }
-                }
+                for (int plane = 0; plane < 2; ++plane)
+                    *reinterpret_cast<u32x2*>(lds_at(r, (k >> 5) * 8 + plane * 4 + (k >> 3 & 3)) + 2 * (k & 4)) = h[i][j].p[plane];
             }
         }
+    __syncthreads();
+    if constexpr (PART == kLast) {
+        const int tensor = block / sink.blocks;
+        const int64_t at0 = (int64_t)(block - tensor * sink.blocks) * sink.m * sink.n;
+        T* out = (T*)sink.out[tensor] + at0;
+        float* master = OUT == kMasters ? sink.master[tensor] + at0 : nullptr;
+        for (int t = threadIdx.x; t < C::BN * PIECES; t += C::THREADS) {
+            const int r = t / PIECES, u = t % PIECES, n = tb * C::BN + r, m = ta * C::BM + 4 * u;
+            if (n >= p.b_rows || m >= p.a_rows) continue;
+            const f32x4 x = *reinterpret_cast<const f32x4*>(lds_at(r, u));
+            const int64_t at = (int64_t)n * sink.n + m;
+            if ((sink.n & 3) == 0) {
+                put4<T, OUT>(sink, out + at, OUT == kMasters ? master + at : nullptr, x);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (m + e < p.a_rows) put<T, OUT>(sink, out + at + e, OUT == kMasters ? master + at + e : nullptr, x[e]);
+            }
+        }
+    } else {
+        const auto leave = [&](int row0, int rows, int col0) {
+            uint16_t* to = p.rows + (int64_t)block * rows * p.rows_half;
+            for (int t = threadIdx.x; t < C::BN * PIECES; t += C::THREADS) {
+                const int r = t / PIECES, u = t % PIECES;
+                const uint32_t at = (uint32_t)col0 * 2 + 8 * u;
+                if (row0 + r < rows && at < p.rows_half) *reinterpret_cast<u32x4*>(to + (int64_t)(row0 + r) * p.rows_half + at) = lds128(lds_at(r, u));
+            }
+        };
+        leave(tb * C::BN, p.b_rows, ta * C::BM);
+        if (HALF && ta != tb) {  // the other side of the diagonal
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < C::TJ; ++j)
+#pragma unroll
+                for (int i = 0; i < C::TI; ++i) {
+                    const int r = mw + 16 * i + (lane & 3), k = (nw & ~3) + 16 * j;
+#pragma unroll
+                    for (int plane = 0; plane < 2; ++plane)
+                        *reinterpret_cast<u32x2*>(lds_at(r, (k >> 5) * 8 + plane * 4 + (k >> 3 & 3)) + 2 * (k & 4)) = change_places(h[i][j].p[plane]);
+                }
+            __syncthreads();
+            leave(ta * C::BM, p.a_rows, tb * C::BN);
+        }
+    }
 }
 
 // ---- small blocks: the whole of it in one launch ----

@@ -78,6 +78,7 @@ enum {
                                      R and L, left there by an earlier monarch_fwd_ws call for the same
                                      shape without this flag; the pack pass is skipped (weights that stay
                                      fixed over many calls: inference, several micro-batches per update) */
+#define MONARCH_FLAG_SKIP_IGNORED 16u /* monarch_xent_fwd: nothing is computed for ignored rows, their lse may be anything */
 
 /* Forward: y = x M^T  (Section 3.3 steps 1-3; one fused pass, the intermediate
  * Y1/U never leaves the chip).  x (batch, n_in), R (k, q, n_in/k), L (k, s, q),
@@ -355,7 +356,8 @@ int monarch_project(const void* A, void* R, void* L, int n, int m,
  * A row whose target is `ignore_index` has no loss (0; its lse is written all the same); a target that is neither that nor
  * an entry of the vocabulary gives NaN.  Products are accumulated in fp32; fp32 operands lose less than 2^-21 of each product.
  * All pointers are device pointers, 16-byte aligned (loss, lse and target: 8).  `workspace` (256-byte aligned) holds
- * monarch_xent_fwd_workspace_bytes(...) bytes; contents ignored on entry.  flags must be 0.  rows == 0 is a successful no-op.
+ * monarch_xent_fwd_workspace_bytes(...) bytes; contents ignored on entry.  flags: MONARCH_FLAG_SKIP_IGNORED only
+ * (what a training step takes: the backward needs nothing of ignored rows).  rows == 0 is a successful no-op.
  * rows, vocab <= 2^20 and width <= 65536, else MONARCH_ERR_UNSUPPORTED. */
 int monarch_xent_fwd(const void* x, const void* W, const int64_t* target, float* loss, float* lse,
                      int64_t rows, int vocab, int width, int64_t ignore_index,

@@ -29,6 +29,7 @@ MONARCH_FLAG_WGRAD_F32 = 1
 MONARCH_FLAG_PERM_B = 2
 MONARCH_FLAG_GENERIC = 4
 MONARCH_FLAG_WS_PACKED = 8
+MONARCH_FLAG_SKIP_IGNORED = 16
 
 # every symbol include/monarch.h declares
 EXPORTS = (
@@ -407,10 +408,12 @@ def monarch_xent_bwd_workspace_bytes(rows: int, vocab: int, width: int, dtype: i
 
 
 def monarch_xent_fwd(x: torch.Tensor, W: torch.Tensor, target: torch.Tensor, loss: torch.Tensor | None = None,
-                     lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None, ignore_index: int = -100, stream=None):
+                     lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None, ignore_index: int = -100, flags: int = 0,
+                     stream=None):
     """(loss, lse), fp32 (rows,): the cross entropy of the logits x W^T against `target` (int64), and the log of the sum of their
-    exponentials.  x (rows, width), W (vocab, width).  Rows whose target is `ignore_index` have loss 0."""
-    return _native_calls.xent_fwd(x, W, target, loss, lse, workspace, ignore_index, stream)
+    exponentials.  x (rows, width), W (vocab, width).  Rows whose target is `ignore_index` have loss 0
+    (with MONARCH_FLAG_SKIP_IGNORED nothing is computed for them, and their lse may be anything)."""
+    return _native_calls.xent_fwd(x, W, target, loss, lse, workspace, ignore_index, flags, stream)
 
 
 def monarch_xent_bwd(x: torch.Tensor, W: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,

@@ -711,17 +711,19 @@ bool xent_pointers(const void* x, const void* W, const int64_t* target, const fl
 
 size_t monarch_xent_fwd_workspace_bytes(int64_t rows, int vocab, int width, monarch_dtype dtype, unsigned flags)
 {
-    return check_xent(rows, vocab, width, (int)dtype, flags, 0u) ? 0 : xent_fwd_workspace(rows, vocab, width, (int)dtype);
+    if (check_xent(rows, vocab, width, (int)dtype, flags, MONARCH_FLAG_SKIP_IGNORED)) return 0;
+    return xent_fwd_workspace(rows, vocab, width, (int)dtype, flags & MONARCH_FLAG_SKIP_IGNORED);
 }
 
 int monarch_xent_fwd(const void* x, const void* W, const int64_t* target, float* loss, float* lse, int64_t rows, int vocab, int width,
                      int64_t ignore_index, monarch_dtype dtype, void* stream, void* workspace, size_t workspace_bytes, unsigned flags)
 {
-    if (int rc = check_xent(rows, vocab, width, (int)dtype, flags, 0u)) return rc;
+    if (int rc = check_xent(rows, vocab, width, (int)dtype, flags, MONARCH_FLAG_SKIP_IGNORED)) return rc;
+    const bool skip = flags & MONARCH_FLAG_SKIP_IGNORED;
     if (rows == 0) return W ? MONARCH_OK : MONARCH_ERR_INVALID;
     if (!xent_pointers(x, W, target, lse) || !loss || !aligned(loss, 8)) return MONARCH_ERR_INVALID;
-    if (!room_for(workspace, workspace_bytes, xent_fwd_workspace(rows, vocab, width, (int)dtype))) return MONARCH_ERR_WORKSPACE;
-    return xent_fwd(x, W, target, loss, lse, rows, vocab, width, ignore_index, (int)dtype, workspace, (hipStream_t)stream);
+    if (!room_for(workspace, workspace_bytes, xent_fwd_workspace(rows, vocab, width, (int)dtype, skip))) return MONARCH_ERR_WORKSPACE;
+    return xent_fwd(x, W, target, loss, lse, rows, vocab, width, ignore_index, (int)dtype, skip, workspace, (hipStream_t)stream);
 }
 
 size_t monarch_xent_bwd_workspace_bytes(int64_t rows, int vocab, int width, monarch_dtype dtype, unsigned flags)

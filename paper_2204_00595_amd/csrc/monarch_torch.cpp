@@ -509,19 +509,19 @@ struct VocabShape {  // x (rows, width), W (vocab, width), target (rows,)
 struct RowLoss {
     Tensor loss, lse;
 };
-RowLoss xent_fwd(const Tensor& x, const Tensor& W, const Tensor& target, RowLoss r, Tensor ws, int64_t ignore, const StreamArg& st)
+RowLoss xent_fwd(const Tensor& x, const Tensor& W, const Tensor& target, RowLoss r, Tensor ws, int64_t ignore, unsigned flags, const StreamArg& st)
 {
     const Where w(x.device(), st);
     const VocabShape sh(x, W, target);
     r.loss = out(r.loss, "loss", {sh.rows}, at::kFloat, sh.device);
     r.lse = out(r.lse, "lse", {sh.rows}, at::kFloat, sh.device);
     if (!ws.defined()) {
-        const size_t need = monarch_xent_fwd_workspace_bytes(sh.rows, (int)sh.vocab, (int)sh.width, sh.code(), 0);
+        const size_t need = monarch_xent_fwd_workspace_bytes(sh.rows, (int)sh.vocab, (int)sh.width, sh.code(), flags);
         if (need) ws = w.scratch(need);
     }
     const Bytes b(ws);
     const int rc = monarch_xent_fwd(ptr(x), ptr(W), target.data_ptr<int64_t>(), (float*)ptr(r.loss), (float*)ptr(r.lse), sh.rows, (int)sh.vocab,
-                                    (int)sh.width, ignore, sh.code(), w.stream(), b.p, b.n, 0);
+                                    (int)sh.width, ignore, sh.code(), w.stream(), b.p, b.n, flags);
     if (rc) raise_status(rc, "monarch_xent_fwd");
     return r;
 }
@@ -591,7 +591,7 @@ struct VocabLossFn : torch::autograd::Function<VocabLossFn> {
         for (const int64_t n : leading) rows *= n;
         const Tensor x2 = dense(x.reshape({rows, x.size(-1)})), W2 = dense(W), t2 = dense(target.reshape({rows}));
         const StreamArg current;
-        const RowLoss r = xent_fwd(x2, W2, t2, {}, {}, ignore, current);
+        const RowLoss r = xent_fwd(x2, W2, t2, {}, {}, ignore, MONARCH_FLAG_SKIP_IGNORED, current);
         const Tensor total = reduction == kNone ? Tensor() : xent_total(r.loss, t2, ignore, reduction == kMean, current);
         ctx->save_for_backward({x2, W2, t2, r.lse, reduction == kMean ? total.slice(0, 1, 2) : Tensor()});
         ctx->saved_data["ignore"] = ignore;
@@ -873,13 +873,14 @@ int64_t int_arg(PyObject* o)
     return v;
 }
 
-// xent_fwd(x, W, target, loss, lse, workspace, ignore_index, stream)
-MONARCH_CALL(py_xent_fwd, 8)
+// xent_fwd(x, W, target, loss, lse, workspace, ignore_index, flags, stream)
+MONARCH_CALL(py_xent_fwd, 9)
     const Tensor x = tensor_arg(a[0], "x"), W = tensor_arg(a[1], "W"), target = tensor_arg(a[2], "target"), ws = optional_arg(a[5], "workspace");
     const RowLoss to{optional_arg(a[3], "loss"), optional_arg(a[4], "lse")};
     const int64_t ignore = int_arg(a[6]);
-    const StreamArg st = stream_arg(a[7]);
-    const RowLoss r = unlocked([&] { return xent_fwd(x, W, target, to, ws, ignore, st); });
+    const unsigned flags = flags_arg(a[7]);
+    const StreamArg st = stream_arg(a[8]);
+    const RowLoss r = unlocked([&] { return xent_fwd(x, W, target, to, ws, ignore, flags, st); });
     return tuple_of({r.loss, r.lse});
 MONARCH_END
 

@@ -62,6 +62,15 @@ __device__ __forceinline__ void store_planes(uint16_t* at, const float (&v)[8], 
     if constexpr (PLANES) *reinterpret_cast<u32x4*>(at + 32) = lo;
 }
 
+// The rows that count, where ignored ones are left out: row i of the operands is row at[i] of x for i < *count; at[*count ..] are the ignored ones.
+struct Counted {
+    const int* at = nullptr;     // null: every row, in its place
+    const int* count = nullptr;
+    const int* target = nullptr; // of the rows that count; -1: outside the vocabulary
+    __device__ __forceinline__ int64_t rows(int64_t all) const { return at ? *count : all; }
+    __device__ __forceinline__ int64_t row(int64_t i) const { return at ? at[i] : i; }
+};
+
 constexpr int kTops = 1024;  // workgroups, at most, that leave the largest magnitude they met
 
 // Largest finite magnitude of `n` values (a workgroup of 256).
@@ -77,17 +86,25 @@ __device__ __forceinline__ float largest_of(const float* __restrict__ v, int n)
 }
 
 // A wave a row: the largest magnitude of src, or with dl of dl[row] src -> tops[workgroup].  With `dst`, the rows as an operand too.
-// bf16: copied, zeros up to whole steps.  fp32: two planes, the row's inverse power of two in inv[row].
+// bf16: copied, zeros up to whole steps.  fp32: two planes, the row's inverse power of two in inv[row].  `zero` (may be null): the ignored rows of
+// it become zero.
 template <typename T>
-__global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, int64_t rows, int width, uint16_t* __restrict__ dst,
+__global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, int64_t all_rows, Counted counted, int width, uint16_t* __restrict__ dst,
                                                    uint32_t row_half, float* __restrict__ inv, const float* __restrict__ dl,
-                                                   float* __restrict__ tops)
+                                                   float* __restrict__ tops, T* __restrict__ zero)
 {
     __shared__ float part[4];
     const int lane = threadIdx.x & 63;
+    const int64_t rows = counted.rows(all_rows);
     float all = 0.f;
-    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += (int64_t)gridDim.x * 4) {
-        const T* s = src + row * width;
+    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < all_rows; row += (int64_t)gridDim.x * 4) {
+        const int64_t from = counted.row(row);
+        if (row >= rows) {
+            if (zero)
+                for (int k = lane; k < width; k += 64) zero[from * width + k] = 0;
+            continue;
+        }
+        const T* s = src + from * width;
         float m = 0.f;
         if (sizeof(T) == 2 && (width & 7) == 0) {
             for (int k = lane * 8; k < width; k += 512) {
@@ -115,7 +132,11 @@ __global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, in
         if (!dst) continue;
         uint16_t* d = dst + row * (int64_t)row_half;
         if constexpr (sizeof(T) == 2) {
-            for (uint32_t k = lane; k < row_half; k += 64) d[k] = k < (uint32_t)width ? s[k] : (uint16_t)0;
+            if ((width & 7) == 0)
+                for (uint32_t k = lane * 8; k < row_half; k += 512)
+                    *reinterpret_cast<u32x4*>(d + k) = k < (uint32_t)width ? ldg128(s + k) : u32x4{0, 0, 0, 0};
+            else
+                for (uint32_t k = lane; k < row_half; k += 64) d[k] = k < (uint32_t)width ? s[k] : (uint16_t)0;
         } else {
             const float up = scale_for(m);
             if (lane == 0) inv[row] = inverse_power(up);
@@ -144,7 +165,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, in
 // Columns of src (rows x width) as rows of an operand of binary16 planes, 64 x 64 at a time, times the power of two for the largest of
 // tops[0 .. n_tops), which goes to *top.  `dl` (may be null): each row times its dl; rows with dl = 0 count as zeros, whatever they hold.
 template <typename T>
-__global__ __launch_bounds__(256) void columns_kernel(const T* __restrict__ src, int64_t rows, int width, uint16_t* __restrict__ dst,
+__global__ __launch_bounds__(256) void columns_kernel(const T* __restrict__ src, int64_t all_rows, Counted counted, int width, uint16_t* __restrict__ dst,
                                                       uint32_t row_half, const float* __restrict__ dl, const float* __restrict__ tops, int n_tops,
                                                       float* __restrict__ top)
 {
@@ -153,15 +174,16 @@ __global__ __launch_bounds__(256) void columns_kernel(const T* __restrict__ src,
     const int tid = threadIdx.x;
     const float largest = largest_of(tops, n_tops), up = scale_for(largest);
     if (blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) *top = largest;
-    const int64_t k0 = (int64_t)blockIdx.x * 64;
+    const int64_t rows = counted.rows(all_rows), k0 = (int64_t)blockIdx.x * 64;
     const int c0 = blockIdx.y * 64;
+    if (k0 >= rows && counted.at) return;  // (steps that no product takes)
     if (sizeof(T) == 2 && (width & 7) == 0) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int r = i * 32 + (tid >> 3), c = (tid & 7) * 8;
             u32x4 u = {0, 0, 0, 0};
             const float by = dl && k0 + r < rows ? dl[k0 + r] : 1.f;
-            if (k0 + r < rows && c0 + c < width && by != 0.f) u = ldg128(src + (k0 + r) * width + c0 + c);
+            if (k0 + r < rows && c0 + c < width && by != 0.f) u = ldg128(src + counted.row(k0 + r) * width + c0 + c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) tile[r][c + e] = by * __uint_as_float(e & 1 ? u[e >> 1] & 0xffff0000u : u[e >> 1] << 16);
         }
@@ -171,7 +193,7 @@ __global__ __launch_bounds__(256) void columns_kernel(const T* __restrict__ src,
             const int r = i * 4 + (tid >> 6), c = tid & 63;
             float v = 0.f;
             const float by = dl && k0 + r < rows ? dl[k0 + r] : 1.f;
-            if (k0 + r < rows && c0 + c < width && by != 0.f) v = by * Elem<T>::load(src + (k0 + r) * width + c0 + c);
+            if (k0 + r < rows && c0 + c < width && by != 0.f) v = by * Elem<T>::load(src + counted.row(k0 + r) * width + c0 + c);
             tile[r][c] = v;
         }
     }
@@ -195,13 +217,15 @@ struct Logits {
     NtOperand w, x;
     const float *winv, *xinv;  // two planes: inverse powers of two of their rows
     const int64_t* target;
-    int64_t rows;
+    int64_t all_rows;
+    Counted counted;
     int vocab, steps, tail;
-    int v0, tiles_v, tiles_t;  // the piece of the vocabulary: entries v0 .. of it
+    int v0, tiles_v;           // the piece of the vocabulary: entries v0 .. of it
+    __device__ __forceinline__ int64_t rows() const { return counted.rows(all_rows); }
 };
 
 template <typename C, bool TAIL>
-__device__ __forceinline__ void logits_tile(const Logits& p, int64_t v0, int64_t t0, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ])
+__device__ __forceinline__ void logits_tile(const Logits& p, int64_t rows, int64_t v0, int64_t t0, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ])
 {
     nt_product<C, TAIL>(p.w, v0, p.x, t0, 0, p.steps, lds, acc, p.tail);
     if constexpr (C::PL == 2) {
@@ -210,7 +234,7 @@ __device__ __forceinline__ void logits_tile(const Logits& p, int64_t v0, int64_t
 #pragma unroll
         for (int j = 0; j < C::TJ; ++j) {
             const int64_t t = t0 + C::col0() + 16 * j + (lane & 15);
-            xi[j] = t < p.rows ? p.xinv[t] : 0.f;
+            xi[j] = t < rows ? p.xinv[t] : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < C::TI; ++i)
@@ -226,9 +250,9 @@ __device__ __forceinline__ void logits_tile(const Logits& p, int64_t v0, int64_t
 
 // Where the target of row t lies among the tile's entries (negative or BM and more: elsewhere).
 template <typename C>
-__device__ __forceinline__ int target_at(const Logits& p, int64_t t, int64_t v0)
+__device__ __forceinline__ int target_at(const Logits& p, int64_t rows, int64_t t, int64_t v0)
 {
-    const int64_t at = t < p.rows ? p.target[t] - v0 : -1;
+    const int64_t at = t >= rows ? -1 : (p.counted.at ? p.counted.target[t] : p.target[t]) - v0;
     return at < 0 || at >= C::BM || v0 + at >= p.vocab ? -C::BM : (int)at;
 }
 
@@ -245,10 +269,11 @@ __global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* 
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int tv, tt;
-    if (!nt_place(blockIdx.x, p.tiles_v, p.tiles_t, tv, tt)) return;
+    const int64_t rows = p.rows();
+    if (!nt_place(blockIdx.x, p.tiles_v, (int)((rows + C::BN - 1) / C::BN), tv, tt)) return;
     const int64_t v0 = (int64_t)tv * C::BM, t0 = (int64_t)tt * C::BN;
     f32x4 acc[C::TI][C::TJ];
-    logits_tile<C, TAIL>(p, v0, t0, lds, acc);
+    logits_tile<C, TAIL>(p, rows, v0, t0, lds, acc);
     const int lane = threadIdx.x & 63;
     const int vr = C::row0() + 4 * (lane >> 4);
     f32x2* red = reinterpret_cast<f32x2*>(lds);  // [BM / WM][BN]
@@ -266,7 +291,7 @@ __global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* 
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j) {
         const int64_t t = t0 + C::col0() + 16 * j + (lane & 15);
-        const int at = target_at<C>(p, t, v0) - vr;  // the target among the lane's entries
+        const int at = target_at<C>(p, rows, t, v0) - vr;  // the target among the lane's entries
         const bool mine = at >= 0 && at < C::WM && (at & 15) < 4;
         if (__any(mine)) {  // (one tile of the vocabulary holds a row's target)
             float l = 0.f;
@@ -297,7 +322,7 @@ __global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* 
     __syncthreads();
     for (int c = threadIdx.x; c < C::BN; c += C::THREADS) {
         const int64_t t = t0 + c;
-        if (t >= p.rows) break;
+        if (t >= rows) break;
         f32x2 r = red[c];
 #pragma unroll
         for (int k = 1; k < C::BM / C::WM; ++k) r = joined(r, red[k * C::BN + c]);
@@ -308,11 +333,11 @@ __global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* 
 // The parts of a row together: one wave a row.
 __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2* __restrict__ part, int parts, const float* __restrict__ hit,
                                                         const int64_t* __restrict__ target, int64_t ignore, int vocab, int64_t rows,
-                                                        float* __restrict__ loss, float* __restrict__ lse)
+                                                        Counted counted, float* __restrict__ loss, float* __restrict__ lse)
 {
     const int lane = threadIdx.x & 63;
     const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (t >= rows) return;
+    if (t >= counted.rows(rows)) return;
     const f32x2* p = part + t * parts;
     float m = -__builtin_inff();
     for (int i = lane; i < parts; i += 64) m = fmaxf(m, p[i][0]);
@@ -323,68 +348,93 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2* __restrict_
     s = wave_all(s, sum_of);
     if (lane) return;
     const float all = (base + log2_fast(s)) * kLn2;
-    const int64_t at = target[t];
+    const int64_t row = counted.row(t), at = target[row];
     float l = 0.f;
     if (at != ignore) l = at >= 0 && at < vocab ? all - hit[t] : __builtin_nanf("");
-    lse[t] = all;
-    loss[t] = l;
+    lse[row] = all;
+    loss[row] = l;
 }
 
 // ---- backward ----
 
-// Upstream gradient of each row -> dl: zero where ignored, NaN where the target is none.
-__global__ __launch_bounds__(256) void xent_upstream_kernel(const float* __restrict__ dloss, int64_t stride, const float* __restrict__ divisor,
-                                                            const int64_t* __restrict__ target, int64_t ignore, int vocab, int64_t rows,
-                                                            float* __restrict__ dl)
+// Which rows count (one workgroup).  Forward (dl null): the others' loss and lse become 0.  Backward: the upstream gradient of the rows that
+// count -> dl, NaN where the target is none, and their lse -> lse_of.
+__global__ __launch_bounds__(1024) void xent_counted_kernel(const int64_t* __restrict__ target, int64_t ignore, int vocab, int64_t rows,
+                                                            int* __restrict__ at, int* __restrict__ target_of, int* __restrict__ count,
+                                                            float* __restrict__ loss, float* lse, const float* __restrict__ dloss, int64_t stride,
+                                                            const float* __restrict__ divisor, float* __restrict__ dl, float* __restrict__ lse_of)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows) return;
-    const int64_t at = target[i];
-    float g = dloss[i * stride] * (divisor ? 1.f / *divisor : 1.f);
-    if (at == ignore) g = 0.f;
-    else if (at < 0 || at >= vocab) g = __builtin_nanf("");
-    dl[i] = g;
+    __shared__ int of_wave[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float by = divisor ? 1.f / *divisor : 1.f;
+    int before = 0;  // rows that count before this round's
+    for (int64_t i0 = 0; i0 < rows; i0 += 1024) {
+        const int64_t i = i0 + threadIdx.x;
+        const int64_t t = i < rows ? target[i] : ignore;
+        const bool counts = t != ignore;
+        const uint64_t all = __ballot(counts);
+        __syncthreads();
+        if (lane == 0) of_wave[wave] = __popcll(all);
+        __syncthreads();
+        int place = before + __popcll(all & (((uint64_t)1 << lane) - 1));
+        for (int w = 0; w < 16; ++w) {
+            place += w < wave ? of_wave[w] : 0;
+            before += of_wave[w];
+        }
+        if (counts) {
+            const bool none = t < 0 || t >= vocab;
+            at[place] = (int)i;
+            target_of[place] = none ? -1 : (int)t;
+            if (dl) {
+                dl[place] = none ? __builtin_nanf("") : dloss[i * stride] * by;
+                lse_of[place] = lse[i];
+            }
+        } else if (i < rows) {
+            at[rows - 1 - (i - place)] = (int)i;  // (from the end on)
+            if (!dl) loss[i] = lse[i] = 0.f;
+        }
+    }
+    if (threadIdx.x == 0) *count = before;
 }
 
 constexpr float kG = 0x1p14f;  // what exp(l - lse) - [v = target] is stored times
 
 // G of a piece of the vocabulary as an operand of binary16 planes, without the upstream gradient; leaves by way of LDS in runs of 64 bytes and
-// more.  Entries and rows that do not exist, and rows that do not count, are written as zeros.
+// more.  Entries and rows that do not exist are written as zeros.
 template <typename C, bool TAIL>
-__global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const float* __restrict__ lse, const float* __restrict__ dl,
-                                                               uint16_t* __restrict__ g, uint32_t g_half)
+__global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const float* __restrict__ lse, uint16_t* __restrict__ g, uint32_t g_half)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int tv, tt;
-    if (!nt_place(blockIdx.x, p.tiles_v, p.tiles_t, tv, tt)) return;
+    const int64_t rows = p.rows();
+    if (!nt_place(blockIdx.x, p.tiles_v, (int)((rows + C::BN - 1) / C::BN), tv, tt)) return;
     const int64_t v0 = p.v0 + (int64_t)tv * C::BM, t0 = (int64_t)tt * C::BN;
     f32x4 acc[C::TI][C::TJ];
-    logits_tile<C, TAIL>(p, v0, t0, lds, acc);
+    logits_tile<C, TAIL>(p, rows, v0, t0, lds, acc);
     const int tid = threadIdx.x, lane = tid & 63;
     const int vr = C::row0() + 4 * (lane >> 4), tc = C::col0() + (lane & 15);
     const int left = p.vocab - v0 - vr < C::BM ? (int)(p.vocab - v0) - vr : C::BM;
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j) {
         const int64_t t = t0 + tc + 16 * j;
-        const bool row = t < p.rows;
+        const bool row = t < rows;
         const float ls = row ? lse[t] : 0.f;
-        const bool counts = row && dl[t] != 0.f;  // (NaN counts)
 #pragma unroll
         for (int i = 0; i < C::TI; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[i][j][e] = exp2_fast((acc[i][j][e] - ls) * kLog2e);
-        const int at = target_at<C>(p, t, v0) - vr;
+        const int at = target_at<C>(p, rows, t, v0) - vr;
         if (__any(at >= 0 && at < C::WM)) {
 #pragma unroll
             for (int i = 0; i < C::TI; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] = at == 16 * i + e ? acc[i][j][e] - 1.f : acc[i][j][e];
         }
-        if (__any(!counts) || left < C::WM) {  // rows that do not count, entries that do not exist
+        if (__any(!row) || left < C::WM) {
 #pragma unroll
             for (int i = 0; i < C::TI; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = !counts || 16 * i + e >= left ? 0.f : acc[i][j][e];
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = !row || 16 * i + e >= left ? 0.f : acc[i][j][e];
         }
     }
     // 16-byte piece u of LDS row r in place u ^ (r % 16)
@@ -420,24 +470,28 @@ struct Unscale {
 };
 
 // out[n][m] (rows of ld) = what A[m] B[n] add up to over the steps, unscaled, as OUT; or, with `part`, as it is to part[z] (+ what lies
-// there), a share of the steps each.  KB: B lies across k, and n counts its columns.
-template <typename C, bool KB, typename OUT>
-__global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, NtOperand bn, int64_t rows, int tiles_m, int tiles_n, int steps,
-                                                                  int shares, OUT* out, int64_t ld, float* part, int add, Unscale by)
+// there), a share of the steps each.  DX: n runs over the rows of x that count and out has all of them; else B lies across k, k runs over the
+// rows of x that count, and n over B's columns.
+template <typename C, bool DX, typename OUT>
+__global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, NtOperand bn, int64_t all_rows, Counted counted, int tiles_m,
+                                                                  int64_t depth, int shares, OUT* out, int64_t ld, float* part, int add, Unscale by)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int tm, tn;
     // (the shares of a tile follow one another on other XCDs; those of neighbouring tiles lie together)
     const int tiles8 = (int)gridDim.x / shares, share = (int)blockIdx.x / tiles8;
-    if (!nt_place((int)blockIdx.x - share * tiles8, tiles_m, tiles_n, tm, tn)) return;
+    const int64_t rows = DX ? counted.rows(all_rows) : all_rows;
+    if (!nt_place((int)blockIdx.x - share * tiles8, tiles_m, (int)((rows + C::BN - 1) / C::BN), tm, tn)) return;
+    constexpr int STEP = C::PL == 2 ? 32 : 64;
+    const int steps = (int)(((DX ? depth : counted.rows(depth)) + STEP - 1) / STEP);
     const int each = (steps + shares - 1) / shares, first = share * each, count = steps - first < each ? steps - first : each;
     f32x4 acc[C::TI][C::TJ];
-    nt_product<C, false, false, KB>(am, (int64_t)tm * C::BM, bn, (int64_t)tn * C::BN, first, count, lds, acc);
+    nt_product<C, false, false, !DX>(am, (int64_t)tm * C::BM, bn, (int64_t)tn * C::BN, first, count, lds, acc);
     const int lane = threadIdx.x & 63;
     const int64_t m0 = (int64_t)tm * C::BM + C::row0() + 4 * (lane >> 4), n0 = (int64_t)tn * C::BN + C::col0() + (lane & 15);
     const bool whole = (ld & 3) == 0;
     const float f = part ? 1.f : by.both();
-    float* sum = part ? part + (int64_t)share * rows * ld : nullptr;
+    float* sum = part ? part + (int64_t)share * all_rows * ld : nullptr;
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j) {
         const int64_t n = n0 + 16 * j;
@@ -450,7 +504,7 @@ __global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, 
             f32x4 v = acc[i][j];
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = v[e] * f * row;
-            const int64_t at = n * ld + m;
+            const int64_t at = (DX && !part ? counted.row(n) : n) * ld + m;
             if (whole) {
                 if (sum) *reinterpret_cast<f32x4*>(sum + at) = add ? v + *reinterpret_cast<const f32x4*>(sum + at) : v;
                 else if constexpr (sizeof(OUT) == 4) *reinterpret_cast<f32x4*>(out + at) = v;
@@ -469,15 +523,29 @@ __global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, 
 
 // The shares together, in order: out = unscaled sum of part[0 .. shares).
 template <typename OUT>
-__global__ __launch_bounds__(256) void xent_shares_kernel(const float* __restrict__ part, int shares, int64_t rows, int64_t ld, OUT* __restrict__ out,
-                                                          Unscale by)
+__global__ __launch_bounds__(256) void xent_shares_kernel(const float* __restrict__ part, int shares, int64_t all_rows, Counted counted, int64_t ld,
+                                                          OUT* __restrict__ out, Unscale by)
 {
-    const int64_t size = rows * ld;
+    const int64_t size = all_rows * ld, rows = counted.rows(all_rows);
     const float f = by.both();
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
+    if ((ld & 3) == 0) {
+        const int64_t quads = ld >> 2;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * quads; i += (int64_t)gridDim.x * 256) {
+            f32x4 s = *reinterpret_cast<const f32x4*>(part + 4 * i);
+            for (int k = 1; k < shares; ++k) s += *reinterpret_cast<const f32x4*>(part + k * size + 4 * i);
+            const int64_t row = i / quads;
+            s = s * f * (by.row ? by.row[row] : 1.f);
+            OUT* to = out + counted.row(row) * ld + 4 * (i - row * quads);
+            if constexpr (sizeof(OUT) == 4) *reinterpret_cast<f32x4*>(to) = s;
+            else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+        }
+        return;
+    }
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * ld; i += (int64_t)gridDim.x * 256) {
         float s = part[i];
         for (int k = 1; k < shares; ++k) s += part[k * size + i];
-        Elem<OUT>::store(out + i, s * f * (by.row ? by.row[i / ld] : 1.f));
+        const int64_t row = i / ld;
+        Elem<OUT>::store(out + counted.row(row) * ld + (i - row * ld), s * f * (by.row ? by.row[row] : 1.f));
     }
 }
 
@@ -548,10 +616,12 @@ struct Plan {
     int per_step() const { return f32 ? 32 : 64; }  // numbers along k in a step
     uint32_t half(int64_t k) const { return (uint32_t)((k + per_step() - 1) / per_step() * 64); }  // 16-bit numbers of an operand's row
     bool forward;  // else the gradients
+    bool skips;    // ignored rows are left out
     // Up to 64 rows the forward of fp32 tensors is bound by reading W, and the fp32 matrix instruction keeps up with that.
     bool plain32() const { return f32 && forward && rows <= 64 && width % 4 == 0; }
-    // rows of whole 16-byte pieces serve as they are
+    // rows of whole 16-byte pieces serve as they are, those of x where none is left out
     bool packs() const { return f32 ? !plain32() : width % 8 != 0; }
+    bool packs_x() const { return packs() || skips; }
     // tile of the logits: 0 = 256 x 256, 1 = 128 x 128, 2 = 128 entries x 64 rows, 3 = 128 x 32 (forward)
     int tile() const { return rows > 128 ? 0 : rows > 64 ? 1 : rows > 32 || !forward ? 2 : 3; }
     int bv() const { return tile() == 0 ? 256 : 128; }
@@ -576,8 +646,8 @@ struct Sides {  // x and W as operands, with their powers of two
     float *xinv = nullptr, *winv = nullptr;
     void lay(const Plan& p, Area& a)
     {
+        if (p.packs_x()) x = a.take<uint16_t>((size_t)p.rows * p.half(p.width));
         if (!p.packs()) return;
-        x = a.take<uint16_t>((size_t)p.rows * p.half(p.width));
         w = a.take<uint16_t>((size_t)p.vocab * p.half(p.width));
         if (!p.f32) return;
         xinv = a.take<float>(p.rows);
@@ -585,14 +655,27 @@ struct Sides {  // x and W as operands, with their powers of two
     }
 };
 
+struct CountedArea {
+    int *at, *target, *count;
+    void lay(const Plan& p, Area& a)
+    {
+        at = p.skips ? a.take<int>(p.rows) : nullptr;
+        target = p.skips ? a.take<int>(p.rows) : nullptr;
+        count = p.skips ? a.take<int>(1) : nullptr;
+    }
+    Counted rows() const { return Counted{at, count, target}; }
+};
+
 struct FwdArea {
     Sides sides;
+    CountedArea counted;
     f32x2* part;
     float* hit;
     size_t lay(const Plan& p, char* base)
     {
         Area a{base};
         sides.lay(p, a);
+        counted.lay(p, a);
         part = a.take<f32x2>((size_t)p.rows * p.parts());
         hit = a.take<float>(p.rows);
         return a.used;
@@ -629,8 +712,9 @@ constexpr size_t kPieceBytes = (size_t)1 << 29;  // G of a piece of the vocabula
 
 struct BwdArea {
     Sides sides;
+    CountedArea counted;
     uint16_t *wt, *xt, *g;
-    float *dl, *top, *tops, *dx_part, *dw_part;  // top: largest of x (times dl) and W; tops: of workgroups, x then W
+    float *lse, *dl, *top, *tops, *dx_part, *dw_part;  // top: largest of x (times dl) and W; tops: of workgroups, x then W
     int piece;                                   // entries of the vocabulary, whole tiles
     Cut dx_cut, dw_cut, dw_last;                 // of a whole piece, and of the last one
     uint32_t g_half, wt_half, xt_half;
@@ -639,6 +723,8 @@ struct BwdArea {
     {
         Area a{base};
         sides.lay(p, a);
+        counted.lay(p, a);
+        lse = a.take<float>(p.rows);
         const int64_t tokens = p.row_tiles() * p.bt();
         piece = (int)tiles_of_piece * p.bv();
         const int per = p.per_step(), last = p.vocab % piece ? p.vocab % piece : piece, first = p.vocab < piece ? p.vocab : piece;
@@ -679,46 +765,45 @@ struct BwdArea {
 int launched() { return hip_status(hipGetLastError()); }
 
 int rows_grid(int64_t rows) { return (int)((rows + 3) / 4 < kTops ? (rows + 3) / 4 : kTops); }
-// Rows of x (rows) or W (vocab) as an operand, where they do not serve as they are, and (tops) the largest magnitudes.
+// Rows of x and W as operands, where they do not serve as they are, and (tops) the largest magnitudes.
 template <typename T>
-int run_rows(const void* src, int64_t rows, int width, uint16_t* dst, uint32_t half, float* inv, const float* dl, float* tops, hipStream_t st)
+int run_rows(const Plan& p, const Sides& s, const Counted& counted, const void* x, const void* w, const float* dl, float* tops, void* dx, hipStream_t st)
 {
-    rows_kernel<T><<<rows_grid(rows), 256, 0, st>>>((const T*)src, rows, width, dst, half, inv, dl, tops);
+    const uint32_t half = p.half(p.width);
+    if (p.packs_x() || tops)
+        rows_kernel<T><<<rows_grid(p.rows), 256, 0, st>>>((const T*)x, p.rows, counted, p.width, s.x, half, s.xinv, dl, tops, (T*)dx);
+    if (p.packs() || tops)
+        rows_kernel<T><<<rows_grid(p.vocab), 256, 0, st>>>((const T*)w, p.vocab, Counted{}, p.width, s.w, half, s.winv, nullptr,
+                                                           tops ? tops + kTops : nullptr, nullptr);
     return launched();
 }
-int pack_sides(const Plan& p, const Sides& s, const void* x, const void* w, const float* dl, float* tops, hipStream_t st)
+int pack_sides(const Plan& p, const Sides& s, const Counted& counted, const void* x, const void* w, const float* dl, float* tops, void* dx, hipStream_t st)
 {
-    if (!p.packs() && !tops) return 0;
-    const uint32_t half = p.half(p.width);
-    float* wtops = tops ? tops + kTops : nullptr;
-    if (p.f32) {
-        if (int rc = run_rows<float>(x, p.rows, p.width, s.x, half, s.xinv, dl, tops, st)) return rc;
-        return run_rows<float>(w, p.vocab, p.width, s.w, half, s.winv, nullptr, wtops, st);
-    }
-    if (int rc = run_rows<uint16_t>(x, p.rows, p.width, s.x, half, nullptr, dl, tops, st)) return rc;
-    return run_rows<uint16_t>(w, p.vocab, p.width, s.w, half, nullptr, nullptr, wtops, st);
+    return p.f32 ? run_rows<float>(p, s, counted, x, w, dl, tops, dx, st) : run_rows<uint16_t>(p, s, counted, x, w, dl, tops, dx, st);
 }
 
-Logits logits_of(const Plan& p, const Sides& s, const void* x, const void* w, const int64_t* target)
+Logits logits_of(const Plan& p, const Sides& s, const Counted& counted, const void* x, const void* w, const int64_t* target)
 {
-    const uint32_t bytes = p.packs() ? p.half(p.width) * 2 : (uint32_t)p.width * (p.f32 ? 4 : 2);
+    const uint32_t whole = p.half(p.width) * 2, plain = (uint32_t)p.width * (p.f32 ? 4 : 2), bytes = p.packs() ? whole : plain;
     Logits l;
     l.w = NtOperand{p.packs() ? s.w : w, p.vocab, bytes};
-    l.x = NtOperand{p.packs() ? s.x : x, p.rows, bytes};
+    l.x = NtOperand{p.packs_x() ? s.x : x, p.rows, p.packs_x() ? whole : plain};
     l.winv = s.winv;
     l.xinv = s.xinv;
     l.target = target;
-    l.rows = p.rows;
+    l.all_rows = p.rows;
+    l.counted = counted;
     l.vocab = p.vocab;
     l.steps = (int)((bytes + 127) / 128);
     l.tail = (int)(bytes % 128 / 16);
     if (!l.tail) l.tail = 8;
     l.v0 = 0;
     l.tiles_v = p.parts();
-    l.tiles_t = (int)p.row_tiles();
     return l;
 }
 
+template <typename C>
+int tiles_of(const Logits& l) { return (int)((l.all_rows + C::BN - 1) / C::BN); }
 // Rows that end inside a step have kernels of their own (the test for it in every step costs 14 % of a long product).
 template <typename C, bool TAIL>
 int run_part(const Logits& l, f32x2* part, int parts, float* hit, hipStream_t st)
@@ -726,47 +811,50 @@ int run_part(const Logits& l, f32x2* part, int parts, float* hit, hipStream_t st
     if constexpr (!TAIL && C::KIND != kF16x2)
         if (l.tail < 8) return run_part<C, true>(l, part, parts, hit, st);
     if (allow_dynamic_lds((const void*)xent_part_kernel<C, TAIL>, C::LDS_BYTES) != hipSuccess) return -4;
-    xent_part_kernel<C, TAIL><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, part, parts, hit);
+    xent_part_kernel<C, TAIL><<<nt_grid(l.tiles_v, tiles_of<C>(l)), C::THREADS, C::LDS_BYTES, st>>>(l, part, parts, hit);
     return launched();
 }
 template <typename C, bool TAIL>
-int run_grad(const Logits& l, const float* lse, const BwdArea& a, hipStream_t st)
+int run_grad(const Logits& l, const BwdArea& a, hipStream_t st)
 {
     if constexpr (!TAIL && C::KIND != kF16x2)
-        if (l.tail < 8) return run_grad<C, true>(l, lse, a, st);
+        if (l.tail < 8) return run_grad<C, true>(l, a, st);
     if (allow_dynamic_lds((const void*)xent_grad_kernel<C, TAIL>, C::LDS_BYTES) != hipSuccess) return -4;
-    xent_grad_kernel<C, TAIL><<<nt_grid(l.tiles_v, l.tiles_t), C::THREADS, C::LDS_BYTES, st>>>(l, lse, a.dl, a.g, a.g_half);
+    xent_grad_kernel<C, TAIL><<<nt_grid(l.tiles_v, tiles_of<C>(l)), C::THREADS, C::LDS_BYTES, st>>>(l, a.lse, a.g, a.g_half);
     return launched();
 }
 
-struct Job {  // out (rows x a.rows, rows of ld) from operands a and b
+struct Job {  // out (rows x a.rows, rows of ld) from operands a and b, `depth` numbers each
     NtOperand a, b;
-    int64_t rows;
-    int steps;
+    int64_t rows, depth;
+    Counted counted;
     void* out;
     int64_t ld;
     float* part;  // where the shares go (null: one share, straight to out)
     bool add, last;
     Unscale by;
 };
-template <typename C, bool KB, typename OUT>
+template <typename C, bool DX, typename OUT>
 int run_product(const Job& j, int shares, hipStream_t st)
 {
-    if (allow_dynamic_lds((const void*)xent_product_kernel<C, KB, OUT>, C::LDS_BYTES) != hipSuccess) return -4;
+    if (allow_dynamic_lds((const void*)xent_product_kernel<C, DX, OUT>, C::LDS_BYTES) != hipSuccess) return -4;
     const int tm = (int)((j.a.rows + C::BM - 1) / C::BM), tn = (int)((j.rows + C::BN - 1) / C::BN);
-    xent_product_kernel<C, KB, OUT><<<nt_grid(tm, tn) * shares, C::THREADS, C::LDS_BYTES, st>>>(j.a, j.b, j.rows, tm, tn, j.steps, shares,
+    xent_product_kernel<C, DX, OUT><<<nt_grid(tm, tn) * shares, C::THREADS, C::LDS_BYTES, st>>>(j.a, j.b, j.rows, j.counted, tm, j.depth, shares,
                                                                                                 (OUT*)j.out, j.ld, j.part, j.add, j.by);
     return launched();
 }
-template <typename B, typename M, bool KB, typename OUT>
+template <typename B, typename M, bool DX, typename OUT>
 int product(const Job& j, const Cut& cut, hipStream_t st)
 {
-    if (int rc = cut.big ? run_product<B, KB, OUT>(j, cut.shares, st) : run_product<M, KB, OUT>(j, cut.shares, st)) return rc;
+    if (int rc = cut.big ? run_product<B, DX, OUT>(j, cut.shares, st) : run_product<M, DX, OUT>(j, cut.shares, st)) return rc;
     if (!j.part || !j.last) return 0;
     const int64_t size = j.rows * j.ld, groups = (size + 1023) / 1024;
-    xent_shares_kernel<OUT><<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(j.part, cut.shares, j.rows, j.ld, (OUT*)j.out, j.by);
+    xent_shares_kernel<OUT><<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(j.part, cut.shares, j.rows, DX ? j.counted : Counted{}, j.ld, (OUT*)j.out, j.by);
     return launched();
 }
+
+// The forward of few rows takes them all: what it has to read is W.
+bool skips(int64_t rows, bool skip) { return skip && rows > 128; }
 
 }  // namespace
 
@@ -775,87 +863,92 @@ bool xent_supported(int64_t rows, int vocab, int width)
     return rows <= (1 << 20) && vocab <= (1 << 20) && width <= (1 << 16);
 }
 
-size_t xent_fwd_workspace(int64_t rows, int vocab, int width, int dtype)
+size_t xent_fwd_workspace(int64_t rows, int vocab, int width, int dtype, bool skip)
 {
     FwdArea a;
-    return rows ? a.lay(Plan{dtype == 0, rows, vocab, width, true}, nullptr) : 0;
+    return rows ? a.lay(Plan{dtype == 0, rows, vocab, width, true, skips(rows, skip)}, nullptr) : 0;
 }
 size_t xent_bwd_workspace(int64_t rows, int vocab, int width, int dtype)
 {
     BwdArea a;
-    return rows ? a.fit(Plan{dtype == 0, rows, vocab, width, false}, nullptr, (size_t)-1) : 0;
+    return rows ? a.fit(Plan{dtype == 0, rows, vocab, width, false, true}, nullptr, (size_t)-1) : 0;
 }
 size_t xent_bwd_least(int64_t rows, int vocab, int width, int dtype)
 {
     BwdArea a;
-    return rows ? a.lay(Plan{dtype == 0, rows, vocab, width, false}, nullptr, 1) : 0;
+    return rows ? a.lay(Plan{dtype == 0, rows, vocab, width, false, true}, nullptr, 1) : 0;
 }
 
 int xent_fwd(const void* x, const void* w, const int64_t* target, float* loss, float* lse, int64_t rows, int vocab, int width, int64_t ignore,
-             int dtype, void* ws, hipStream_t st)
+             int dtype, bool skip, void* ws, hipStream_t st)
 {
-    const Plan p{dtype == 0, rows, vocab, width, true};
+    const Plan p{dtype == 0, rows, vocab, width, true, skips(rows, skip)};
     FwdArea a;
     a.lay(p, (char*)ws);
-    if (int rc = pack_sides(p, a.sides, x, w, nullptr, nullptr, st)) return rc;
-    const Logits l = logits_of(p, a.sides, x, w, target);
+    const Counted counted = a.counted.rows();
+    if (p.skips)
+        xent_counted_kernel<<<1, 1024, 0, st>>>(target, ignore, vocab, rows, a.counted.at, a.counted.target, a.counted.count, loss, lse, nullptr, 0, nullptr,
+                                                nullptr, nullptr);
+    int rc = pack_sides(p, a.sides, counted, x, w, nullptr, nullptr, nullptr, st);
+    if (rc) return rc;
+    const Logits l = logits_of(p, a.sides, counted, x, w, target);
     const int parts = p.parts();
-    int rc;
     if (p.plain32()) rc = p.rows > 32 ? run_part<Low32, false>(l, a.part, parts, a.hit, st) : run_part<Few32, false>(l, a.part, parts, a.hit, st);
     else if (p.f32) rc = by_tile<Big2, Mid2, Low2, Few2>(p, [&](auto c) { return run_part<decltype(c), false>(l, a.part, parts, a.hit, st); });
     else rc = by_tile<Big, Mid, Low, FewB>(p, [&](auto c) { return run_part<decltype(c), false>(l, a.part, parts, a.hit, st); });
     if (rc) return rc;
-    xent_join_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a.part, parts, a.hit, target, ignore, vocab, rows, loss, lse);
+    xent_join_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a.part, parts, a.hit, target, ignore, vocab, rows, counted, loss, lse);
     return launched();
 }
 
 int xent_bwd(const void* x, const void* w, const int64_t* target, const float* lse, const float* dloss, int64_t dloss_stride, const float* divisor,
              void* dx, void* dw, int64_t rows, int vocab, int width, int64_t ignore, int dtype, bool dw_f32, void* ws, size_t ws_bytes, hipStream_t st)
 {
-    const Plan p{dtype == 0, rows, vocab, width, false};
+    const Plan p{dtype == 0, rows, vocab, width, false, true};
     BwdArea a;
     if (!a.fit(p, (char*)ws, ws_bytes)) return -3;
-    xent_upstream_kernel<<<(unsigned)((rows + 255) / 256), 256, 0, st>>>(dloss, dloss_stride, divisor, target, ignore, vocab, rows, a.dl);
-    if (int rc = launched()) return rc;
-    if (int rc = pack_sides(p, a.sides, x, w, a.dl, a.tops, st)) return rc;
+    const Counted counted = a.counted.rows();
+    xent_counted_kernel<<<1, 1024, 0, st>>>(target, ignore, vocab, rows, a.counted.at, a.counted.target, a.counted.count, nullptr, const_cast<float*>(lse),
+                                            dloss, dloss_stride, divisor, a.dl, a.lse);
+    int rc = pack_sides(p, a.sides, counted, x, w, a.dl, a.tops, dx, st);
+    if (rc) return rc;
     const unsigned columns = (unsigned)((width + 63) / 64);
-    auto pack_columns = [&](const void* src, int64_t n, uint16_t* to, uint32_t half, const float* dl, const float* tops, float* top) {
+    auto pack_columns = [&](const void* src, int64_t n, const Counted& of, uint16_t* to, uint32_t half, const float* dl, const float* tops, float* top) {
         const dim3 grid((unsigned)((half / (p.f32 ? 2 : 1) + 63) / 64), columns);
-        if (p.f32) columns_kernel<float><<<grid, 256, 0, st>>>((const float*)src, n, width, to, half, dl, tops, rows_grid(n), top);
-        else columns_kernel<uint16_t><<<grid, 256, 0, st>>>((const uint16_t*)src, n, width, to, half, dl, tops, rows_grid(n), top);
+        if (p.f32) columns_kernel<float><<<grid, 256, 0, st>>>((const float*)src, n, of, width, to, half, dl, tops, rows_grid(n), top);
+        else columns_kernel<uint16_t><<<grid, 256, 0, st>>>((const uint16_t*)src, n, of, width, to, half, dl, tops, rows_grid(n), top);
         return launched();
     };
-    int rc = 0;
-    if (dx && (rc = pack_columns(w, vocab, a.wt, a.wt_half, nullptr, a.tops + kTops, a.top + 1))) return rc;
-    if (dw && (rc = pack_columns(x, rows, a.xt, a.xt_half, a.dl, a.tops, a.top))) return rc;
-    Logits l = logits_of(p, a.sides, x, w, target);
+    if (dx && (rc = pack_columns(w, vocab, Counted{}, a.wt, a.wt_half, nullptr, a.tops + kTops, a.top + 1))) return rc;
+    if (dw && (rc = pack_columns(x, rows, counted, a.xt, a.xt_half, a.dl, a.tops, a.top))) return rc;
+    Logits l = logits_of(p, a.sides, counted, x, w, target);
     const int per = p.per_step();
     for (int v0 = 0; v0 < vocab; v0 += a.piece) {
         const int entries = a.entries_of(p, v0);
         const bool last = v0 + a.piece >= vocab;
         l.v0 = v0;
         l.tiles_v = (entries + p.bv() - 1) / p.bv();
-        if (p.f32) rc = by_tile<Big2, Mid2, Low2, Low2>(p, [&](auto c) { return run_grad<decltype(c), false>(l, lse, a, st); });
-        else rc = by_tile<Big, Mid, Low, Low>(p, [&](auto c) { return run_grad<decltype(c), false>(l, lse, a, st); });
+        if (p.f32) rc = by_tile<Big2, Mid2, Low2, Low2>(p, [&](auto c) { return run_grad<decltype(c), false>(l, a, st); });
+        else rc = by_tile<Big, Mid, Low, Low>(p, [&](auto c) { return run_grad<decltype(c), false>(l, a, st); });
         if (rc) return rc;
         if (dx) {
             // features inside, rows of x outside
-            Job j{{a.wt + (size_t)v0 / per * 64, width, a.wt_half * 2}, {a.g, rows, a.g_half * 2}, rows, (entries + per - 1) / per, dx, width,
-                  a.dx_part, v0 > 0, last, {a.top + 1, a.dl}};
-            rc = p.f32 ? product<Big2, Mid2, false, float>(j, a.dx_cut, st) : product<Big16, Mid16, false, uint16_t>(j, a.dx_cut, st);
+            Job j{{a.wt + (size_t)v0 / per * 64, width, a.wt_half * 2}, {a.g, rows, a.g_half * 2}, rows, entries, counted, dx, width, a.dx_part,
+                  v0 > 0, last, {a.top + 1, a.dl}};
+            rc = p.f32 ? product<Big2, Mid2, true, float>(j, a.dx_cut, st) : product<Big16, Mid16, true, uint16_t>(j, a.dx_cut, st);
             if (rc) return rc;
         }
         if (dw) {
             const Cut& cut = last ? a.dw_last : a.dw_cut;
-            Job j{{a.xt, width, a.xt_half * 2}, {a.g, rows, a.g_half * 2}, entries, (int)((rows + per - 1) / per), nullptr, width,
+            Job j{{a.xt, width, a.xt_half * 2}, {a.g, rows, a.g_half * 2}, entries, rows, counted, nullptr, width,
                   cut.shares > 1 ? a.dw_part : nullptr, false, true, {a.top, nullptr}};
             const size_t at = (size_t)v0 * width;
             if (dw_f32) {
                 j.out = (float*)dw + at;
-                rc = p.f32 ? product<Big2, Mid2, true, float>(j, cut, st) : product<Big16, Mid16, true, float>(j, cut, st);
+                rc = p.f32 ? product<Big2, Mid2, false, float>(j, cut, st) : product<Big16, Mid16, false, float>(j, cut, st);
             } else {
                 j.out = (uint16_t*)dw + at;
-                rc = product<Big16, Mid16, true, uint16_t>(j, cut, st);
+                rc = product<Big16, Mid16, false, uint16_t>(j, cut, st);
             }
             if (rc) return rc;
         }

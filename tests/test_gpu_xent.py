@@ -305,3 +305,21 @@ def test_refusals(ops):
         binding.monarch_xent_bwd(x, W, target, lse, torch.ones(3, device="cuda"))
     with pytest.raises(TypeError):
         binding.monarch_xent_bwd(x, W, target, lse, torch.ones(8, device="cuda").bfloat16())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, ignored", [(40, 0.5), (200, 0.0), (1500, 0.4), (3000, 0.95), (300, 1.0)])
+def test_ignored_rows_left_out(ops, dtype, rows, ignored):
+    """The forward that computes nothing for them gives the losses, and the lse of the others, of the one that does."""
+    _, binding = ops
+    x, W, target = inputs(rows, 450, 72, dtype, ignored=ignored)
+    x[target == IGNORE] = float("nan")
+    want = Exact(x, W, target, torch.ones(rows), dtype)
+    xd, Wd, td = x.cuda(), W.cuda(), target.cuda()
+    loss, lse = binding.monarch_xent_fwd(xd, Wd, td, flags=binding.MONARCH_FLAG_SKIP_IGNORED)
+    counts = target != IGNORE
+    within(loss, want.loss, want.row_bound, "loss")
+    within(lse.cpu()[counts], want.lse[counts], want.row_bound, "lse")
+    dx, dW = binding.monarch_xent_bwd(xd, Wd, td, lse, torch.ones(rows, device="cuda"))
+    within(dx, want.dx, want.dx_bound, "dx")
+    within(dW, want.dW, want.dW_bound, "dW")

@@ -85,6 +85,18 @@ __device__ __forceinline__ float largest_of(const float* __restrict__ v, int n)
     return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
 }
 
+// bf16 numbers k .. k + 7 of a row that may start anywhere; zeros from `width` on
+__device__ __forceinline__ u32x4 eight_of(const uint16_t* row, int k, int width)
+{
+    typedef u32x4 __attribute__((aligned(2))) loose;
+    if (k + 8 <= width) return *reinterpret_cast<const loose*>(row + k);
+    u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (k + e < width) v[e >> 1] |= (uint32_t)row[k + e] << (16 * (e & 1));
+    return v;
+}
+
 // A wave a row: the largest magnitude of src, or with dl of dl[row] src -> tops[workgroup].  With `dst`, the rows as an operand too.
 // bf16: copied, zeros up to whole steps.  fp32: two planes, the row's inverse power of two in inv[row].  `zero` (may be null): the ignored rows of
 // it become zero.
@@ -106,9 +118,9 @@ __global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, in
         }
         const T* s = src + from * width;
         float m = 0.f;
-        if (sizeof(T) == 2 && (width & 7) == 0) {
+        if constexpr (sizeof(T) == 2) {
             for (int k = lane * 8; k < width; k += 512) {
-                const u32x4 u = ldg128(s + k);
+                const u32x4 u = eight_of(s, k, width);
                 uint32_t t = 0;  // (magnitudes of bf16 numbers are in the order of their bits)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -132,11 +144,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, in
         if (!dst) continue;
         uint16_t* d = dst + row * (int64_t)row_half;
         if constexpr (sizeof(T) == 2) {
-            if ((width & 7) == 0)
-                for (uint32_t k = lane * 8; k < row_half; k += 512)
-                    *reinterpret_cast<u32x4*>(d + k) = k < (uint32_t)width ? ldg128(s + k) : u32x4{0, 0, 0, 0};
-            else
-                for (uint32_t k = lane; k < row_half; k += 64) d[k] = k < (uint32_t)width ? s[k] : (uint16_t)0;
+            for (uint32_t k = lane * 8; k < row_half; k += 512) *reinterpret_cast<u32x4*>(d + k) = eight_of(s, k, width);
         } else {
             const float up = scale_for(m);
             if (lane == 0) inv[row] = inverse_power(up);
@@ -177,13 +185,13 @@ __global__ __launch_bounds__(256) void columns_kernel(const T* __restrict__ src,
     const int64_t rows = counted.rows(all_rows), k0 = (int64_t)blockIdx.x * 64;
     const int c0 = blockIdx.y * 64;
     if (k0 >= rows && counted.at) return;  // (steps that no product takes)
-    if (sizeof(T) == 2 && (width & 7) == 0) {
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int r = i * 32 + (tid >> 3), c = (tid & 7) * 8;
             u32x4 u = {0, 0, 0, 0};
             const float by = dl && k0 + r < rows ? dl[k0 + r] : 1.f;
-            if (k0 + r < rows && c0 + c < width && by != 0.f) u = ldg128(src + counted.row(k0 + r) * width + c0 + c);
+            if (k0 + r < rows && c0 + c < width && by != 0.f) u = eight_of(src + counted.row(k0 + r) * width, c0 + c, width);
 #pragma unroll
             for (int e = 0; e < 8; ++e) tile[r][c + e] = by * __uint_as_float(e & 1 ? u[e >> 1] & 0xffff0000u : u[e >> 1] << 16);
         }
@@ -622,8 +630,12 @@ struct Plan {
     // rows of whole 16-byte pieces serve as they are, those of x where none is left out
     bool packs() const { return f32 ? !plain32() : width % 8 != 0; }
     bool packs_x() const { return packs() || skips; }
-    // tile of the logits: 0 = 256 x 256, 1 = 128 x 128, 2 = 128 entries x 64 rows, 3 = 128 x 32 (forward)
-    int tile() const { return rows > 128 ? 0 : rows > 64 ? 1 : rows > 32 || !forward ? 2 : 3; }
+    // tile of the logits: 0 = 256 x 256 (where there is one for each CU), 1 = 128 x 128, 2 = 128 entries x 64 rows, 3 = 128 x 32 (forward)
+    int tile() const
+    {
+        if (rows > 128 && ((rows + 255) / 256) * ((vocab + 255) / 256) >= 256) return 0;
+        return rows > 64 ? 1 : rows > 32 || !forward ? 2 : 3;
+    }
     int bv() const { return tile() == 0 ? 256 : 128; }
     int bt() const { return tile() == 0 ? 256 : tile() == 1 ? 128 : tile() == 2 ? 64 : 32; }
     int parts() const { return (vocab + bv() - 1) / bv(); }

@@ -477,6 +477,69 @@ struct Unscale {
     __device__ __forceinline__ float both() const { return inverse_power(scale_for(*top)) * (1.f / kG); }
 };
 
+// Rows of running sums are whole 16-byte pieces.
+__host__ __device__ __forceinline__ int64_t sum_ld(int64_t ld) { return (ld + 3) / 4 * 4; }
+
+// 16 bytes, or the first `count` numbers of them, to wherever a row's numbers start
+__device__ __forceinline__ void leave16(float* to, u32x4 v, int count)
+{
+    typedef u32x4 __attribute__((aligned(4))) loose;
+    if (count >= 4) *reinterpret_cast<loose*>(to) = v;
+    else
+        for (int e = 0; e < 3; ++e)
+            if (e < count) to[e] = __uint_as_float(v[e]);
+}
+__device__ __forceinline__ void leave16(uint16_t* to, u32x4 v, int count)
+{
+    typedef u32x4 __attribute__((aligned(2))) loose;
+    if (count >= 8) *reinterpret_cast<loose*>(to) = v;
+    else
+        for (int e = 0; e < 7; ++e)
+            if (e < count) to[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+}
+
+// A tile of results, times `by` and row[n], to rows n of `ld` numbers each: by way of LDS, as whole lines (a lane holds four numbers of a row and
+// its neighbours other rows').  16-byte piece u of LDS row r in place u ^ (r % 16); fp32 tiles of 256 x 256 go in two halves.
+template <typename C, typename OUT>
+__device__ __forceinline__ void leave(const f32x4 (&acc)[C::TI][C::TJ], unsigned char* lds, OUT* out, const Counted& counted, int64_t n0, int64_t rows,
+                                      int64_t m0, int64_t columns, int64_t ld, bool add, float by, const float* __restrict__ row_by)
+{
+    constexpr int PASSES = C::BM * C::BN * (int)sizeof(OUT) > C::LDS_BYTES ? 2 : 1, COLS = C::BM / PASSES;
+    constexpr int ROW = COLS * (int)sizeof(OUT), PIECES = ROW / 16, EACH = 16 / (int)sizeof(OUT);
+    static_assert(C::BN * ROW <= C::LDS_BYTES && (PASSES == 1 || C::WM == COLS) && PIECES >= 16, "room, and a pass for each row of waves");
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+        __syncthreads();
+        if (PASSES == 1 || C::row0() == pass * COLS) {
+#pragma unroll
+            for (int j = 0; j < C::TJ; ++j) {
+                const int r = C::col0() + 16 * j + (lane & 15);
+                const float f = row_by && n0 + r < rows ? by * row_by[n0 + r] : by;
+#pragma unroll
+                for (int i = 0; i < C::TI; ++i) {
+                    const int m = C::row0() - pass * COLS + 16 * i + 4 * (lane >> 4);
+                    const f32x4 v = acc[i][j] * f;
+                    unsigned char* at = lds + r * ROW + 16 * ((m / EACH) ^ (r & 15));
+                    if constexpr (sizeof(OUT) == 4) *reinterpret_cast<f32x4*>(at) = v;
+                    else *reinterpret_cast<u32x2*>(at + 2 * (m & 4)) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                }
+            }
+        }
+        __syncthreads();
+        for (int t = threadIdx.x; t < C::BN * PIECES; t += C::THREADS) {
+            const int r = t / PIECES, u = t % PIECES;
+            const int64_t n = n0 + r, m = m0 + pass * COLS + u * EACH;
+            if (n >= rows || m >= columns) continue;
+            u32x4 v = lds128(lds + r * ROW + 16 * (u ^ (r & 15)));
+            OUT* to = out + counted.row(n) * ld + m;
+            if constexpr (sizeof(OUT) == 4)  // (a sum's rows are whole pieces)
+                if (add) v = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, v) + *reinterpret_cast<const f32x4*>(to));
+            leave16(to, v, columns - m < EACH && !add ? (int)(columns - m) : EACH);
+        }
+    }
+}
+
 // out[n][m] (rows of ld) = what A[m] B[n] add up to over the steps, unscaled, as OUT; or, with `part`, as it is to part[z] (+ what lies
 // there), a share of the steps each.  DX: n runs over the rows of x that count and out has all of them; else B lies across k, k runs over the
 // rows of x that count, and n over B's columns.
@@ -495,38 +558,9 @@ __global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, 
     const int each = (steps + shares - 1) / shares, first = share * each, count = steps - first < each ? steps - first : each;
     f32x4 acc[C::TI][C::TJ];
     nt_product<C, false, false, !DX>(am, (int64_t)tm * C::BM, bn, (int64_t)tn * C::BN, first, count, lds, acc);
-    const int lane = threadIdx.x & 63;
-    const int64_t m0 = (int64_t)tm * C::BM + C::row0() + 4 * (lane >> 4), n0 = (int64_t)tn * C::BN + C::col0() + (lane & 15);
-    const bool whole = (ld & 3) == 0;
-    const float f = part ? 1.f : by.both();
-    float* sum = part ? part + (int64_t)share * all_rows * ld : nullptr;
-#pragma unroll
-    for (int j = 0; j < C::TJ; ++j) {
-        const int64_t n = n0 + 16 * j;
-        if (n >= rows) continue;
-        const float row = !part && by.row ? by.row[n] : 1.f;
-#pragma unroll
-        for (int i = 0; i < C::TI; ++i) {
-            const int64_t m = m0 + 16 * i;
-            if (m >= am.rows) continue;
-            f32x4 v = acc[i][j];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = v[e] * f * row;
-            const int64_t at = (DX && !part ? counted.row(n) : n) * ld + m;
-            if (whole) {
-                if (sum) *reinterpret_cast<f32x4*>(sum + at) = add ? v + *reinterpret_cast<const f32x4*>(sum + at) : v;
-                else if constexpr (sizeof(OUT) == 4) *reinterpret_cast<f32x4*>(out + at) = v;
-                else *reinterpret_cast<u32x2*>(out + at) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (m + e >= am.rows) break;
-                    if (sum) sum[at + e] = add ? v[e] + sum[at + e] : v[e];
-                    else Elem<OUT>::store(out + at + e, v[e]);
-                }
-            }
-        }
-    }
+    if (part) leave<C, float>(acc, lds, part + (int64_t)share * all_rows * sum_ld(ld), Counted{}, (int64_t)tn * C::BN, rows, (int64_t)tm * C::BM,
+                               am.rows, sum_ld(ld), add, 1.f, nullptr);
+    else leave<C, OUT>(acc, lds, out, DX ? counted : Counted{}, (int64_t)tn * C::BN, rows, (int64_t)tm * C::BM, am.rows, ld, false, by.both(), by.row);
 }
 
 // The shares together, in order: out = unscaled sum of part[0 .. shares).
@@ -534,26 +568,22 @@ template <typename OUT>
 __global__ __launch_bounds__(256) void xent_shares_kernel(const float* __restrict__ part, int shares, int64_t all_rows, Counted counted, int64_t ld,
                                                           OUT* __restrict__ out, Unscale by)
 {
-    const int64_t size = all_rows * ld, rows = counted.rows(all_rows);
+    const int64_t quads = sum_ld(ld) >> 2, size = all_rows * 4 * quads, rows = counted.rows(all_rows);
     const float f = by.both();
-    if ((ld & 3) == 0) {
-        const int64_t quads = ld >> 2;
-        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * quads; i += (int64_t)gridDim.x * 256) {
-            f32x4 s = *reinterpret_cast<const f32x4*>(part + 4 * i);
-            for (int k = 1; k < shares; ++k) s += *reinterpret_cast<const f32x4*>(part + k * size + 4 * i);
-            const int64_t row = i / quads;
-            s = s * f * (by.row ? by.row[row] : 1.f);
-            OUT* to = out + counted.row(row) * ld + 4 * (i - row * quads);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * quads; i += (int64_t)gridDim.x * 256) {
+        f32x4 s = *reinterpret_cast<const f32x4*>(part + 4 * i);
+        for (int k = 1; k < shares; ++k) s += *reinterpret_cast<const f32x4*>(part + k * size + 4 * i);
+        const int64_t row = i / quads, m = 4 * (i - row * quads);
+        s = s * f * (by.row ? by.row[row] : 1.f);
+        OUT* to = out + counted.row(row) * ld + m;
+        if ((ld & 3) == 0) {
             if constexpr (sizeof(OUT) == 4) *reinterpret_cast<f32x4*>(to) = s;
             else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (m + e < ld) Elem<OUT>::store(to + e, s[e]);
         }
-        return;
-    }
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * ld; i += (int64_t)gridDim.x * 256) {
-        float s = part[i];
-        for (int k = 1; k < shares; ++k) s += part[k * size + i];
-        const int64_t row = i / ld;
-        Elem<OUT>::store(out + counted.row(row) * ld + (i - row * ld), s * f * (by.row ? by.row[row] : 1.f));
     }
 }
 
@@ -753,9 +783,9 @@ struct BwdArea {
         dl = a.take<float>(p.rows);
         top = a.take<float>(2);
         tops = a.take<float>(2 * kTops);
-        dx_part = dx_cut.shares > 1 || several ? a.take<float>((size_t)dx_cut.shares * p.rows * p.width) : nullptr;
+        dx_part = dx_cut.shares > 1 || several ? a.take<float>((size_t)dx_cut.shares * p.rows * sum_ld(p.width)) : nullptr;
         const size_t one = dw_cut.shares > 1 ? (size_t)dw_cut.shares * first : 0, two = dw_last.shares > 1 ? (size_t)dw_last.shares * last : 0;
-        dw_part = one || two ? a.take<float>((one > two ? one : two) * p.width) : nullptr;
+        dw_part = one || two ? a.take<float>((one > two ? one : two) * sum_ld(p.width)) : nullptr;
         return a.used;
     }
     // Pieces as long as kPieceBytes and a workspace of `room` bytes allow, a little shorter where the tiles of dW then fill whole rounds; 0: not even

@@ -365,44 +365,52 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2* __restrict_
 
 // ---- backward ----
 
-// Which rows count (one workgroup).  Forward (dl null): the others' loss and lse become 0.  Backward: the upstream gradient of the rows that
-// count -> dl, NaN where the target is none, and their lse -> lse_of.
+// Which rows count: a workgroup for 1024 of them, which counts those before by itself (16384 rows: 6 us; one workgroup for all of them 20).  Forward (dl
+// null): the others' loss and lse become 0.  Backward: the upstream gradient of the rows that count -> dl, NaN where the target is none, and
+// their lse -> lse_of.
 __global__ __launch_bounds__(1024) void xent_counted_kernel(const int64_t* __restrict__ target, int64_t ignore, int vocab, int64_t rows,
                                                             int* __restrict__ at, int* __restrict__ target_of, int* __restrict__ count,
                                                             float* __restrict__ loss, float* lse, const float* __restrict__ dloss, int64_t stride,
                                                             const float* __restrict__ divisor, float* __restrict__ dl, float* __restrict__ lse_of)
 {
-    __shared__ int of_wave[16];
+    __shared__ int of_wave[2][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float by = divisor ? 1.f / *divisor : 1.f;
-    int before = 0;  // rows that count before this round's
-    for (int64_t i0 = 0; i0 < rows; i0 += 1024) {
-        const int64_t i = i0 + threadIdx.x;
-        const int64_t t = i < rows ? target[i] : ignore;
-        const bool counts = t != ignore;
-        const uint64_t all = __ballot(counts);
-        __syncthreads();
-        if (lane == 0) of_wave[wave] = __popcll(all);
-        __syncthreads();
-        int place = before + __popcll(all & (((uint64_t)1 << lane) - 1));
-        for (int w = 0; w < 16; ++w) {
-            place += w < wave ? of_wave[w] : 0;
-            before += of_wave[w];
-        }
-        if (counts) {
-            const bool none = t < 0 || t >= vocab;
-            at[place] = (int)i;
-            target_of[place] = none ? -1 : (int)t;
-            if (dl) {
-                dl[place] = none ? __builtin_nanf("") : dloss[i * stride] * by;
-                lse_of[place] = lse[i];
-            }
-        } else if (i < rows) {
-            at[rows - 1 - (i - place)] = (int)i;  // (from the end on)
-            if (!dl) loss[i] = lse[i] = 0.f;
-        }
+    const int64_t i0 = (int64_t)blockIdx.x * 1024, i = i0 + threadIdx.x;
+    const int64_t t = i < rows ? target[i] : ignore;
+    float g = 0.f, l = 0.f;
+    if (dl && i < rows) {
+        g = dloss[i * stride] * (divisor ? 1.f / *divisor : 1.f);
+        l = lse[i];
     }
-    if (threadIdx.x == 0) *count = before;
+    int before = 0;
+#pragma unroll 8
+    for (int64_t k = threadIdx.x; k < i0; k += 1024) before += target[k] != ignore;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) before += __shfl_xor(before, d);
+    const uint64_t all = __ballot(t != ignore);
+    if (lane == 0) {
+        of_wave[0][wave] = before;
+        of_wave[1][wave] = __popcll(all);
+    }
+    __syncthreads();
+    int place = __popcll(all & (((uint64_t)1 << lane) - 1)), total = 0;
+    for (int w = 0; w < 16; ++w) {
+        place += of_wave[0][w] + (w < wave ? of_wave[1][w] : 0);
+        total += of_wave[0][w] + of_wave[1][w];
+    }
+    if (t != ignore) {
+        const bool none = t < 0 || t >= vocab;
+        at[place] = (int)i;
+        target_of[place] = none ? -1 : (int)t;
+        if (dl) {
+            dl[place] = none ? __builtin_nanf("") : g;
+            lse_of[place] = l;
+        }
+    } else if (i < rows) {
+        at[rows - 1 - (i - place)] = (int)i;  // (from the end on)
+        if (!dl) loss[i] = lse[i] = 0.f;
+    }
+    if (threadIdx.x == 0 && blockIdx.x + 1 == gridDim.x) *count = total;
 }
 
 constexpr float kG = 0x1p14f;  // what exp(l - lse) - [v = target] is stored times
@@ -593,11 +601,22 @@ __global__ __launch_bounds__(1024) void xent_total_kernel(const float* __restric
 {
     __shared__ double part[2][16];
     double s = 0, c = 0;
-    for (int64_t i = threadIdx.x; i < rows; i += 1024)
-        if (target[i] != ignore) {
-            s += loss[i];
-            c += 1;
+    for (int64_t i = threadIdx.x; i < rows; i += 4096) {
+        int64_t t[4];
+        float l[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t k = i + 1024 * e;
+            t[e] = k < rows ? target[k] : ignore;
+            l[e] = k < rows ? loss[k] : 0.f;
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (t[e] != ignore) {
+                s += l[e];
+                c += 1;
+            }
+    }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
         s += __shfl_xor(s, d);
@@ -929,7 +948,7 @@ int xent_fwd(const void* x, const void* w, const int64_t* target, float* loss, f
     a.lay(p, (char*)ws);
     const Counted counted = a.counted.rows();
     if (p.skips)
-        xent_counted_kernel<<<1, 1024, 0, st>>>(target, ignore, vocab, rows, a.counted.at, a.counted.target, a.counted.count, loss, lse, nullptr, 0, nullptr,
+        xent_counted_kernel<<<(unsigned)((rows + 1023) / 1024), 1024, 0, st>>>(target, ignore, vocab, rows, a.counted.at, a.counted.target, a.counted.count, loss, lse, nullptr, 0, nullptr,
                                                 nullptr, nullptr);
     int rc = pack_sides(p, a.sides, counted, x, w, nullptr, nullptr, nullptr, st);
     if (rc) return rc;
@@ -950,7 +969,7 @@ int xent_bwd(const void* x, const void* w, const int64_t* target, const float* l
     BwdArea a;
     if (!a.fit(p, (char*)ws, ws_bytes)) return -3;
     const Counted counted = a.counted.rows();
-    xent_counted_kernel<<<1, 1024, 0, st>>>(target, ignore, vocab, rows, a.counted.at, a.counted.target, a.counted.count, nullptr, const_cast<float*>(lse),
+    xent_counted_kernel<<<(unsigned)((rows + 1023) / 1024), 1024, 0, st>>>(target, ignore, vocab, rows, a.counted.at, a.counted.target, a.counted.count, nullptr, const_cast<float*>(lse),
                                             dloss, dloss_stride, divisor, a.dl, a.lse);
     int rc = pack_sides(p, a.sides, counted, x, w, a.dl, a.tops, dx, st);
     if (rc) return rc;

@@ -461,3 +461,9 @@ def monarch_muon_step(weights, grads, momenta, lr: float, momentum: float = 0.95
         scale = math.sqrt(max(1.0, weights[0].shape[-2] / weights[0].shape[-1])) if len(weights) else 1.0
     _native_calls.muon_step(weights, grads, momenta, masters, lr, momentum, weight_decay, scale, nesterov, coefficients, steps, eps,
                             workspace, stream)
+
+
+def dense(t: torch.Tensor) -> torch.Tensor:
+    """`t`, or a copy of it that the calls take: contiguous and on 16 bytes."""
+    t = t.contiguous()
+    return t.clone() if t.data_ptr() % 16 else t

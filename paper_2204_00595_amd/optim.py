@@ -1,0 +1,76 @@
+"""The optimiser for Monarch factors (and dense matrices): orthogonalised momenta.
+
+``Muon`` follows the momentum of each parameter's gradient made orthogonal block by block (``monarch_muon_step``): a Monarch factor
+(k, q, p) is a stack of k blocks, and the block-diagonal matrix it stands for gets an update whose singular values are all near 1.  Parameters
+of one shape are stepped together, in a few launches whatever their number.  Vectors (biases, norms) and embeddings belong to another
+optimiser.  No arithmetic here.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding
+
+
+class Muon(torch.optim.Optimizer):
+    """v <- momentum v + grad;  p <- (1 - lr weight_decay) p - lr scale orthogonal(grad + momentum v).
+
+    Parameters have two dimensions, or three (a stack of blocks), fp32 or bf16, contiguous.  ``scale``: sqrt(max(1, rows / columns)) of a block
+    unless given.  bf16 parameters are stepped on fp32 masters, made of them at their first step and kept in the state
+    (``masters=False``: on themselves, which loses updates below their rounding).  Momenta are fp32.  Where a parameter is
+    written from outside between steps, its state must go too (``optimizer.state.pop(parameter)``): the next step writes the master's rounding.
+    """
+
+    def __init__(self, params, lr: float = 0.02, momentum: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
+                 scale: float | None = None, steps: int = 5, coefficients=binding.MUON_COEFFICIENTS, eps: float = 1e-7, masters: bool = True):
+        if lr < 0 or momentum < 0 or weight_decay < 0:
+            raise ValueError("lr, momentum and weight_decay must not be negative")
+        super().__init__(params, dict(lr=lr, momentum=momentum, weight_decay=weight_decay, nesterov=nesterov, scale=scale, steps=steps,
+                                      coefficients=tuple(coefficients), eps=eps, masters=masters))
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        try:
+            for p in self.param_groups[-1]["params"]:
+                if p.dim() not in (2, 3) or p.dtype not in (torch.float32, torch.bfloat16) or not p.is_contiguous():
+                    raise ValueError("Muon takes contiguous matrices, or stacks of them, in float32 or bfloat16; got shape %s of %s"
+                                     % (tuple(p.shape), p.dtype))
+        except ValueError:
+            self.param_groups.pop()
+            raise
+
+    def load_state_dict(self, state_dict):
+        """As the base class, but momenta and masters stay fp32 (which it would round to the parameters' type)."""
+        super().load_state_dict(state_dict)
+        saved = [i for g in state_dict["param_groups"] for i in g["params"]]
+        for i, p in zip(saved, (p for g in self.param_groups for p in g["params"])):
+            if i in state_dict["state"]:
+                self.state[p] = {k: v.detach().to(device=p.device, dtype=torch.float32, copy=True) for k, v in state_dict["state"][i].items()}
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            alike = {}  # parameters that go together
+            for p in group["params"]:
+                if p.grad is None or p.numel() == 0:
+                    continue
+                if p.grad.is_sparse:
+                    raise RuntimeError("Muon takes no sparse gradients")
+                state = self.state[p]
+                if not state:
+                    state["momentum"] = torch.zeros_like(p, dtype=torch.float32)
+                    if group["masters"] and p.dtype == torch.bfloat16:
+                        state["master"] = p.to(torch.float32, copy=True)
+                alike.setdefault((p.shape, p.dtype, p.grad.dtype, p.device, "master" in state), []).append(p)
+            for (_, _, _, device, with_masters), params in alike.items():
+                with torch.cuda.device(device):
+                    binding.monarch_muon_step(
+                        params, [binding.dense(p.grad) for p in params], [self.state[p]["momentum"] for p in params], lr=group["lr"],
+                        momentum=group["momentum"], weight_decay=group["weight_decay"], nesterov=group["nesterov"], scale=group["scale"],
+                        steps=group["steps"], coefficients=group["coefficients"], eps=group["eps"],
+                        masters=[self.state[p]["master"] for p in params] if with_masters else None)
+        return loss

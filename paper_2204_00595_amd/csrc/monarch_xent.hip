@@ -62,7 +62,7 @@ __device__ __forceinline__ void store_planes(uint16_t* at, const float (&v)[8], 
     if constexpr (PLANES) *reinterpret_cast<u32x4*>(at + 32) = lo;
 }
 
-// The rows that count, where ignored ones are left out: row i of the operands is row at[i] of x for i < *count; at[*count ..] are the ignored ones.
+// The rows that count, where ignored ones are left out: row i of the operands is row at[i] of x for i < *count.
 struct Counted {
     const int* at = nullptr;     // null: every row, in its place
     const int* count = nullptr;
@@ -97,92 +97,175 @@ __device__ __forceinline__ u32x4 eight_of(const uint16_t* row, int k, int width)
     return v;
 }
 
-// A wave a row: the largest magnitude of src, or with dl of dl[row] src -> tops[workgroup].  With `dst`, the rows as an operand too.
-// bf16: copied, zeros up to whole steps.  fp32: two planes, the row's inverse power of two in inv[row].  `zero` (may be null): the ignored rows of
-// it become zero.
+// One row, a wave: its largest magnitude; with `d`, as a row of an operand too.  bf16: copied, zeros up to whole steps.  fp32: two planes, the inverse
+// of the row's power of two to *inv.
 template <typename T>
-__global__ __launch_bounds__(256) void rows_kernel(const T* __restrict__ src, int64_t all_rows, Counted counted, int width, uint16_t* __restrict__ dst,
-                                                   uint32_t row_half, float* __restrict__ inv, const float* __restrict__ dl,
-                                                   float* __restrict__ tops, T* __restrict__ zero)
+__device__ __forceinline__ float take_row(const T* __restrict__ s, int width, uint16_t* __restrict__ d, uint32_t row_half, float* __restrict__ inv)
 {
-    __shared__ float part[4];
     const int lane = threadIdx.x & 63;
-    const int64_t rows = counted.rows(all_rows);
-    float all = 0.f;
-    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < all_rows; row += (int64_t)gridDim.x * 4) {
-        const int64_t from = counted.row(row);
-        if (row >= rows) {
-            if (zero)
-                for (int k = lane; k < width; k += 64) zero[from * width + k] = 0;
-            continue;
-        }
-        const T* s = src + from * width;
-        float m = 0.f;
-        if constexpr (sizeof(T) == 2) {
-            for (int k = lane * 8; k < width; k += 512) {
-                const u32x4 u = eight_of(s, k, width);
-                uint32_t t = 0;  // (magnitudes of bf16 numbers are in the order of their bits)
+    float m = 0.f;
+    if constexpr (sizeof(T) == 2) {
+        for (int k = lane * 8; k < width; k += 512) {
+            const u32x4 u = eight_of(s, k, width);
+            uint32_t t = 0;  // (magnitudes of bf16 numbers are in the order of their bits)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t h = (u[e >> 1] >> (16 * (e & 1))) & 0x7fffu;
-                    t = h < 0x7f80u && h > t ? h : t;
-                }
-                m = fmaxf(m, __uint_as_float(t << 16));
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t h = (u[e >> 1] >> (16 * (e & 1))) & 0x7fffu;
+                t = h < 0x7f80u && h > t ? h : t;
             }
-        } else {
-            const int quads = sizeof(T) == 4 && (width & 3) == 0 ? width / 4 : 0;
-            if constexpr (sizeof(T) == 4)
-                for (int k = lane; k < quads; k += 64) {
-                    const f32x4 u = *reinterpret_cast<const f32x4*>(s + 4 * k);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_magnitude(u[e]));
-                }
-            for (int k = 4 * quads + lane; k < width; k += 64) m = fmaxf(m, finite_magnitude(Elem<T>::load(s + k)));
+            m = fmaxf(m, __uint_as_float(t << 16));
         }
-        m = wave_all(m, max_of);
-        all = fmaxf(all, dl ? finite_magnitude(dl[row]) * m : m);
-        if (!dst) continue;
-        uint16_t* d = dst + row * (int64_t)row_half;
-        if constexpr (sizeof(T) == 2) {
-            for (uint32_t k = lane * 8; k < row_half; k += 512) *reinterpret_cast<u32x4*>(d + k) = eight_of(s, k, width);
-        } else {
-            const float up = scale_for(m);
-            if (lane == 0) inv[row] = inverse_power(up);
-            for (uint32_t k = lane * 8; k < row_half / 2; k += 512) {
-                float v[8];
-                if ((width & 3) == 0) {
+    } else {
+        const int quads = (width & 3) == 0 ? width / 4 : 0;
+        for (int k = lane; k < quads; k += 64) {
+            const f32x4 u = *reinterpret_cast<const f32x4*>(s + 4 * k);
 #pragma unroll
-                    for (int e = 0; e < 8; e += 4) {
-                        const f32x4 u = k + e < (uint32_t)width ? *reinterpret_cast<const f32x4*>(s + k + e) : f32x4{0.f, 0.f, 0.f, 0.f};
-                        v[e] = u[0], v[e + 1] = u[1], v[e + 2] = u[2], v[e + 3] = u[3];
-                    }
-                } else {
+            for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_magnitude(u[e]));
+        }
+        for (int k = 4 * quads + lane; k < width; k += 64) m = fmaxf(m, finite_magnitude(s[k]));
+    }
+    m = wave_all(m, max_of);
+    if (!d) return m;
+    if constexpr (sizeof(T) == 2) {
+        for (uint32_t k = lane * 8; k < row_half; k += 512) *reinterpret_cast<u32x4*>(d + k) = eight_of(s, k, width);
+    } else {
+        const float up = scale_for(m);
+        if (lane == 0) *inv = inverse_power(up);
+        for (uint32_t k = lane * 8; k < row_half / 2; k += 512) {
+            float v[8];
+            if ((width & 3) == 0) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = k + e < (uint32_t)width ? s[k + e] : 0.f;
+                for (int e = 0; e < 8; e += 4) {
+                    const f32x4 u = k + e < (uint32_t)width ? *reinterpret_cast<const f32x4*>(s + k + e) : f32x4{0.f, 0.f, 0.f, 0.f};
+                    v[e] = u[0], v[e + 1] = u[1], v[e + 2] = u[2], v[e + 3] = u[3];
                 }
-                store_planes<true>(d + (k >> 5) * 64 + (k & 31), v, up);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = k + e < (uint32_t)width ? s[k + e] : 0.f;
             }
+            store_planes<true>(d + (k >> 5) * 64 + (k & 31), v, up);
         }
     }
+    return m;
+}
+
+template <typename T>
+struct Taken {  // rows to take
+    const T* src;
+    int64_t rows;
+    uint16_t* dst;  // null: no operand
+    float *inv, *tops;  // tops (may be null): the largest magnitude a workgroup met, of x times the rows' dl
+    int groups;     // workgroups for them
+};
+struct Counting {  // the rows of x that count; what is kept of them
+    const int64_t* target;
+    int64_t ignore;
+    int vocab;
+    int *at, *target_of, *count;  // (at null: every row counts)
+    float *loss, *lse;            // forward: those of the other rows become 0
+    const float *dloss, *divisor, *lse_in;  // backward: the upstream gradient -> dl, NaN where the target is none, and the rows' lse -> lse_of
+    int64_t stride;
+    float *dl, *lse_of;
+};
+
+// The rows of x and of W (groups of workgroups beside one another).  Each workgroup of x takes rows that follow one another and counts by
+// itself which of those before them count, so that no launch comes before this one (as launches of their own, three for a forward and three
+// for a backward of 777 rows of width 330, 8191 entries: 10 us more).  `zero` (may be null): the rows of dx that do not count become zero.
+template <typename T>
+__global__ __launch_bounds__(256) void xent_rows_kernel(Taken<T> x, Counting c, Taken<T> w, int width, uint32_t row_half, T* __restrict__ zero)
+{
+    __shared__ float top_of[4];
+    __shared__ int count_of[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = (int)blockIdx.x - x.groups;
+    float all = 0.f;
+    if (group >= 0) {
+        for (int64_t row = (int64_t)group * 4 + wave; row < w.rows; row += (int64_t)w.groups * 4)
+            all = fmaxf(all, take_row(w.src + row * width, width, w.dst ? w.dst + row * (int64_t)row_half : nullptr, row_half, w.inv + row));
+    } else {
+        const int64_t each = (x.rows + x.groups - 1) / x.groups, i = blockIdx.x * each, i0 = i < x.rows ? i : x.rows;
+        const int64_t i1 = i0 + each < x.rows ? i0 + each : x.rows;
+        int64_t place = i0;  // of the next row that counts
+        if (c.at) {
+            int before = 0;
+#pragma unroll 8
+            for (int64_t k = threadIdx.x; k < i0; k += 256) before += c.target[k] != c.ignore;
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1) before += __shfl_xor(before, d);
+            if (lane == 0) count_of[wave] = before;
+            __syncthreads();
+            place = count_of[0] + count_of[1] + count_of[2] + count_of[3];
+        }
+        const float by = c.dl && c.divisor ? 1.f / *c.divisor : 1.f;
+        for (int64_t b = i0; b < i1; b += 64) {
+            const int64_t t = b + lane < i1 ? c.target[b + lane] : c.ignore;
+            const uint64_t counts = c.at ? __ballot(t != c.ignore) : ~(uint64_t)0;
+            for (int r = wave; r < 64 && b + r < i1; r += 4) {
+                const int64_t from = b + r;
+                if (!(counts >> r & 1)) {
+                    if (zero)
+                        for (int k = lane; k < width; k += 64) zero[from * width + k] = 0;
+                    if (c.loss && lane == 0) c.loss[from] = c.lse[from] = 0.f;
+                    continue;
+                }
+                const int64_t to = place + (c.at ? __popcll(counts & (((uint64_t)1 << r) - 1)) : r);
+                float g = 1.f;
+                if (c.at) {
+                    const int64_t is = __shfl(t, r);
+                    const bool none = is < 0 || is >= c.vocab;
+                    if (c.dl) g = none ? __builtin_nanf("") : c.dloss[from * c.stride] * by;
+                    if (lane == 0) {
+                        c.at[to] = (int)from;
+                        c.target_of[to] = none ? -1 : (int)is;
+                        if (c.dl) {
+                            c.dl[to] = g;
+                            c.lse_of[to] = c.lse_in[from];
+                        }
+                    }
+                }
+                const float m = take_row(x.src + from * width, width, x.dst ? x.dst + to * (int64_t)row_half : nullptr, row_half, x.inv + to);
+                all = fmaxf(all, finite_magnitude(g) * m);
+            }
+            place += c.at ? __popcll(counts) : 64;
+        }
+        if (c.at && threadIdx.x == 0 && (int)blockIdx.x + 1 == x.groups) *c.count = (int)place;
+    }
+    float* tops = group >= 0 ? w.tops : x.tops;
     if (!tops) return;
-    if (lane == 0) part[threadIdx.x >> 6] = all;
+    if (lane == 0) top_of[wave] = all;
     __syncthreads();
-    if (threadIdx.x == 0) tops[blockIdx.x] = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+    if (threadIdx.x == 0) tops[group >= 0 ? group : (int)blockIdx.x] = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
 }
 
 // Columns of src (rows x width) as rows of an operand of binary16 planes, 64 x 64 at a time, times the power of two for the largest of
 // tops[0 .. n_tops), which goes to *top.  `dl` (may be null): each row times its dl; rows with dl = 0 count as zeros, whatever they hold.
 template <typename T>
-__global__ __launch_bounds__(256) void columns_kernel(const T* __restrict__ src, int64_t all_rows, Counted counted, int width, uint16_t* __restrict__ dst,
-                                                      uint32_t row_half, const float* __restrict__ dl, const float* __restrict__ tops, int n_tops,
-                                                      float* __restrict__ top)
+struct Turned {
+    const T* src;
+    int64_t rows;
+    Counted counted;
+    uint16_t* dst;
+    uint32_t row_half;
+    const float *dl, *tops;
+    int n_tops;
+    float* top;
+    int tiles;  // of 64 rows
+};
+template <typename T>
+__global__ __launch_bounds__(256) void xent_columns_kernel(Turned<T> one, Turned<T> two, int width)
 {
     constexpr bool kPlanes = sizeof(T) == 4;
     __shared__ float tile[64][65];
-    const int tid = threadIdx.x;
-    const float largest = largest_of(tops, n_tops), up = scale_for(largest);
-    if (blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) *top = largest;
-    const int64_t rows = counted.rows(all_rows), k0 = (int64_t)blockIdx.x * 64;
+    const bool first = (int)blockIdx.x < one.tiles;
+    const Turned<T>& p = first ? one : two;
+    const int tid = threadIdx.x, at = first ? (int)blockIdx.x : (int)blockIdx.x - one.tiles;
+    const T* __restrict__ src = p.src;
+    const float* __restrict__ dl = p.dl;
+    uint16_t* __restrict__ dst = p.dst;
+    const Counted counted = p.counted;
+    const uint32_t row_half = p.row_half;
+    const float largest = largest_of(p.tops, p.n_tops), up = scale_for(largest);
+    if (at == 0 && blockIdx.y == 0 && tid == 0) *p.top = largest;
+    const int64_t rows = counted.rows(p.rows), k0 = (int64_t)at * 64;
     const int c0 = blockIdx.y * 64;
     if (k0 >= rows && counted.at) return;  // (steps that no product takes)
     if constexpr (sizeof(T) == 2) {
@@ -364,54 +447,6 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2* __restrict_
 }
 
 // ---- backward ----
-
-// Which rows count: a workgroup for 1024 of them, which counts those before by itself (16384 rows: 6 us; one workgroup for all of them 20).  Forward (dl
-// null): the others' loss and lse become 0.  Backward: the upstream gradient of the rows that count -> dl, NaN where the target is none, and
-// their lse -> lse_of.
-__global__ __launch_bounds__(1024) void xent_counted_kernel(const int64_t* __restrict__ target, int64_t ignore, int vocab, int64_t rows,
-                                                            int* __restrict__ at, int* __restrict__ target_of, int* __restrict__ count,
-                                                            float* __restrict__ loss, float* lse, const float* __restrict__ dloss, int64_t stride,
-                                                            const float* __restrict__ divisor, float* __restrict__ dl, float* __restrict__ lse_of)
-{
-    __shared__ int of_wave[2][16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t i0 = (int64_t)blockIdx.x * 1024, i = i0 + threadIdx.x;
-    const int64_t t = i < rows ? target[i] : ignore;
-    float g = 0.f, l = 0.f;
-    if (dl && i < rows) {
-        g = dloss[i * stride] * (divisor ? 1.f / *divisor : 1.f);
-        l = lse[i];
-    }
-    int before = 0;
-#pragma unroll 8
-    for (int64_t k = threadIdx.x; k < i0; k += 1024) before += target[k] != ignore;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) before += __shfl_xor(before, d);
-    const uint64_t all = __ballot(t != ignore);
-    if (lane == 0) {
-        of_wave[0][wave] = before;
-        of_wave[1][wave] = __popcll(all);
-    }
-    __syncthreads();
-    int place = __popcll(all & (((uint64_t)1 << lane) - 1)), total = 0;
-    for (int w = 0; w < 16; ++w) {
-        place += of_wave[0][w] + (w < wave ? of_wave[1][w] : 0);
-        total += of_wave[0][w] + of_wave[1][w];
-    }
-    if (t != ignore) {
-        const bool none = t < 0 || t >= vocab;
-        at[place] = (int)i;
-        target_of[place] = none ? -1 : (int)t;
-        if (dl) {
-            dl[place] = none ? __builtin_nanf("") : g;
-            lse_of[place] = l;
-        }
-    } else if (i < rows) {
-        at[rows - 1 - (i - place)] = (int)i;  // (from the end on)
-        if (!dl) loss[i] = lse[i] = 0.f;
-    }
-    if (threadIdx.x == 0 && blockIdx.x + 1 == gridDim.x) *count = total;
-}
 
 constexpr float kG = 0x1p14f;  // what exp(l - lse) - [v = target] is stored times
 
@@ -826,21 +861,31 @@ struct BwdArea {
 int launched() { return hip_status(hipGetLastError()); }
 
 int rows_grid(int64_t rows) { return (int)((rows + 3) / 4 < kTops ? (rows + 3) / 4 : kTops); }
-// Rows of x and W as operands, where they do not serve as they are, and (tops) the largest magnitudes.
+// Which rows count, rows of x and W as operands where they do not serve as they are, and (tops) the largest magnitudes.
 template <typename T>
-int run_rows(const Plan& p, const Sides& s, const Counted& counted, const void* x, const void* w, const float* dl, float* tops, void* dx, hipStream_t st)
+int run_rows(const Plan& p, const Sides& s, const Counting& c, const void* x, const void* w, float* tops, void* dx, hipStream_t st)
 {
-    const uint32_t half = p.half(p.width);
-    if (p.packs_x() || tops)
-        rows_kernel<T><<<rows_grid(p.rows), 256, 0, st>>>((const T*)x, p.rows, counted, p.width, s.x, half, s.xinv, dl, tops, (T*)dx);
-    if (p.packs() || tops)
-        rows_kernel<T><<<rows_grid(p.vocab), 256, 0, st>>>((const T*)w, p.vocab, Counted{}, p.width, s.w, half, s.winv, nullptr,
-                                                           tops ? tops + kTops : nullptr, nullptr);
+    const Taken<T> tx{(const T*)x, p.rows, s.x, s.xinv, tops, p.packs_x() || tops ? rows_grid(p.rows) : 0};
+    const Taken<T> tw{(const T*)w, p.vocab, s.w, s.winv, tops ? tops + kTops : nullptr, p.packs() || tops ? rows_grid(p.vocab) : 0};
+    if (!(tx.groups + tw.groups)) return 0;
+    xent_rows_kernel<T><<<tx.groups + tw.groups, 256, 0, st>>>(tx, c, tw, p.width, p.half(p.width), (T*)dx);
     return launched();
 }
-int pack_sides(const Plan& p, const Sides& s, const Counted& counted, const void* x, const void* w, const float* dl, float* tops, void* dx, hipStream_t st)
+int pack_sides(const Plan& p, const Sides& s, const Counting& c, const void* x, const void* w, float* tops, void* dx, hipStream_t st)
 {
-    return p.f32 ? run_rows<float>(p, s, counted, x, w, dl, tops, dx, st) : run_rows<uint16_t>(p, s, counted, x, w, dl, tops, dx, st);
+    return p.f32 ? run_rows<float>(p, s, c, x, w, tops, dx, st) : run_rows<uint16_t>(p, s, c, x, w, tops, dx, st);
+}
+
+// x^T (times dl) for dW, W^T for dx, as far as they are wanted.
+template <typename T>
+int run_columns(const Plan& p, const BwdArea& a, const Counted& counted, const void* x, bool with_x, const void* w, bool with_w, hipStream_t st)
+{
+    const auto tiles = [&](uint32_t half) { return (int)((half / (p.f32 ? 2 : 1) + 63) / 64); };
+    const Turned<T> tw{(const T*)w, p.vocab, Counted{}, a.wt, a.wt_half, nullptr, a.tops + kTops, rows_grid(p.vocab), a.top + 1, with_w ? tiles(a.wt_half) : 0};
+    const Turned<T> tx{(const T*)x, p.rows, counted, a.xt, a.xt_half, a.dl, a.tops, rows_grid(p.rows), a.top, with_x ? tiles(a.xt_half) : 0};
+    if (!(tw.tiles + tx.tiles)) return 0;
+    xent_columns_kernel<T><<<dim3((unsigned)(tw.tiles + tx.tiles), (unsigned)((p.width + 63) / 64)), 256, 0, st>>>(tw, tx, p.width);
+    return launched();
 }
 
 Logits logits_of(const Plan& p, const Sides& s, const Counted& counted, const void* x, const void* w, const int64_t* target)
@@ -947,10 +992,8 @@ int xent_fwd(const void* x, const void* w, const int64_t* target, float* loss, f
     FwdArea a;
     a.lay(p, (char*)ws);
     const Counted counted = a.counted.rows();
-    if (p.skips)
-        xent_counted_kernel<<<(unsigned)((rows + 1023) / 1024), 1024, 0, st>>>(target, ignore, vocab, rows, a.counted.at, a.counted.target, a.counted.count, loss, lse, nullptr, 0, nullptr,
-                                                nullptr, nullptr);
-    int rc = pack_sides(p, a.sides, counted, x, w, nullptr, nullptr, nullptr, st);
+    Counting c{target, ignore, vocab, a.counted.at, a.counted.target, a.counted.count, loss, lse};
+    int rc = pack_sides(p, a.sides, c, x, w, nullptr, nullptr, st);
     if (rc) return rc;
     const Logits l = logits_of(p, a.sides, counted, x, w, target);
     const int parts = p.parts();
@@ -969,19 +1012,11 @@ int xent_bwd(const void* x, const void* w, const int64_t* target, const float* l
     BwdArea a;
     if (!a.fit(p, (char*)ws, ws_bytes)) return -3;
     const Counted counted = a.counted.rows();
-    xent_counted_kernel<<<(unsigned)((rows + 1023) / 1024), 1024, 0, st>>>(target, ignore, vocab, rows, a.counted.at, a.counted.target, a.counted.count, nullptr, const_cast<float*>(lse),
-                                            dloss, dloss_stride, divisor, a.dl, a.lse);
-    int rc = pack_sides(p, a.sides, counted, x, w, a.dl, a.tops, dx, st);
+    Counting c{target, ignore, vocab, a.counted.at, a.counted.target, a.counted.count, nullptr, nullptr, dloss, divisor, lse, dloss_stride, a.dl, a.lse};
+    int rc = pack_sides(p, a.sides, c, x, w, a.tops, dx, st);
+    if (!rc) rc = p.f32 ? run_columns<float>(p, a, counted, x, dw != nullptr, w, dx != nullptr, st)
+                        : run_columns<uint16_t>(p, a, counted, x, dw != nullptr, w, dx != nullptr, st);
     if (rc) return rc;
-    const unsigned columns = (unsigned)((width + 63) / 64);
-    auto pack_columns = [&](const void* src, int64_t n, const Counted& of, uint16_t* to, uint32_t half, const float* dl, const float* tops, float* top) {
-        const dim3 grid((unsigned)((half / (p.f32 ? 2 : 1) + 63) / 64), columns);
-        if (p.f32) columns_kernel<float><<<grid, 256, 0, st>>>((const float*)src, n, of, width, to, half, dl, tops, rows_grid(n), top);
-        else columns_kernel<uint16_t><<<grid, 256, 0, st>>>((const uint16_t*)src, n, of, width, to, half, dl, tops, rows_grid(n), top);
-        return launched();
-    };
-    if (dx && (rc = pack_columns(w, vocab, Counted{}, a.wt, a.wt_half, nullptr, a.tops + kTops, a.top + 1))) return rc;
-    if (dw && (rc = pack_columns(x, rows, counted, a.xt, a.xt_half, a.dl, a.tops, a.top))) return rc;
     Logits l = logits_of(p, a.sides, counted, x, w, target);
     const int per = p.per_step();
     for (int v0 = 0; v0 < vocab; v0 += a.piece) {

@@ -117,10 +117,14 @@ __device__ __forceinline__ float take_row(const T* __restrict__ s, int width, ui
         }
     } else {
         const int quads = (width & 3) == 0 ? width / 4 : 0;
-        for (int k = lane; k < quads; k += 64) {
-            const f32x4 u = *reinterpret_cast<const f32x4*>(s + 4 * k);
+        for (int k0 = lane; k0 < quads + lane; k0 += 256) {  // (four loads under way; past the end the last quad once more)
+            f32x4 u[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_magnitude(u[e]));
+            for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const f32x4*>(s + 4 * (k0 + 64 * i < quads ? k0 + 64 * i : quads - 1));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_magnitude(u[i][e]));
         }
         for (int k = 4 * quads + lane; k < width; k += 64) m = fmaxf(m, finite_magnitude(s[k]));
     }
@@ -263,8 +267,6 @@ __global__ __launch_bounds__(256) void xent_columns_kernel(Turned<T> one, Turned
     uint16_t* __restrict__ dst = p.dst;
     const Counted counted = p.counted;
     const uint32_t row_half = p.row_half;
-    const float largest = largest_of(p.tops, p.n_tops), up = scale_for(largest);
-    if (at == 0 && blockIdx.y == 0 && tid == 0) *p.top = largest;
     const int64_t rows = counted.rows(p.rows), k0 = (int64_t)at * 64;
     const int c0 = blockIdx.y * 64;
     if (k0 >= rows && counted.at) return;  // (steps that no product takes)
@@ -278,6 +280,20 @@ __global__ __launch_bounds__(256) void xent_columns_kernel(Turned<T> one, Turned
 #pragma unroll
             for (int e = 0; e < 8; ++e) tile[r][c + e] = by * __uint_as_float(e & 1 ? u[e >> 1] & 0xffff0000u : u[e >> 1] << 16);
         }
+    } else if ((width & 3) == 0) {
+        f32x4 v[4];
+        float by[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = i * 16 + (tid >> 4), c = (tid & 15) * 4;
+            by[i] = dl && k0 + r < rows ? dl[k0 + r] : 1.f;
+            v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (k0 + r < rows && c0 + c < width && by[i] != 0.f) v[i] = *reinterpret_cast<const f32x4*>(src + counted.row(k0 + r) * width + c0 + c);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tile[i * 16 + (tid >> 4)][(tid & 15) * 4 + e] = by[i] * v[i][e];
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -288,7 +304,8 @@ __global__ __launch_bounds__(256) void xent_columns_kernel(Turned<T> one, Turned
             tile[r][c] = v;
         }
     }
-    __syncthreads();
+    const float largest = largest_of(p.tops, p.n_tops), up = scale_for(largest);  // (passes a barrier)
+    if (at == 0 && blockIdx.y == 0 && tid == 0) *p.top = largest;
     // eight along k of one column a piece
 #pragma unroll
     for (int i = 0; i < 2; ++i) {

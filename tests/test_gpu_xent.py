@@ -323,3 +323,20 @@ def test_ignored_rows_left_out(ops, dtype, rows, ignored):
     dx, dW = binding.monarch_xent_bwd(xd, Wd, td, lse, torch.ones(rows, device="cuda"))
     within(dx, want.dx, want.dx_bound, "dx")
     within(dW, want.dW, want.dW_bound, "dW")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1025, 4097, 5000, 9001])
+def test_more_rows_than_are_taken_at_once(ops, dtype, rows):
+    """Workgroups that take several rows each, the last ones fewer or none, and some nothing but ignored ones."""
+    x, W, target = inputs(rows, 90, 10, dtype, ignored=0.3)
+    target[1:300] = IGNORE
+    g = torch.rand((rows,), generator=torch.Generator().manual_seed(7)) - 0.3
+    want = Exact(x, W, target, g, dtype)
+    for more in ({}, {"flags": ops[1].MONARCH_FLAG_SKIP_IGNORED}):
+        xd, Wd, td = x.cuda(), W.cuda(), target.cuda()
+        loss, lse = ops[1].monarch_xent_fwd(xd, Wd, td, **more)
+        dx, dW = ops[1].monarch_xent_bwd(xd, Wd, td, lse, g.cuda())
+        within(loss, want.loss, want.row_bound, "loss")
+        within(dx, want.dx, want.dx_bound, "dx")
+        within(dW, want.dW, want.dW_bound, "dW")

@@ -559,14 +559,16 @@ __device__ __forceinline__ void leave16(uint16_t* to, u32x4 v, int count)
 }
 
 // A tile of results, times `by` and row[n], to rows n of `ld` numbers each: by way of LDS, as whole lines (a lane holds four numbers of a row and
-// its neighbours other rows').  16-byte piece u of LDS row r in place u ^ (r % 16); fp32 tiles of 256 x 256 go in two halves.
+// its neighbours other rows').  16-byte piece u of LDS row r in place u ^ (r % 16) (% 8 where the pieces are no multiple of 16); fp32 tiles of 256 rows
+// go in two halves.
 template <typename C, typename OUT>
 __device__ __forceinline__ void leave(const f32x4 (&acc)[C::TI][C::TJ], unsigned char* lds, OUT* out, const Counted& counted, int64_t n0, int64_t rows,
                                       int64_t m0, int64_t columns, int64_t ld, bool add, float by, const float* __restrict__ row_by)
 {
     constexpr int PASSES = C::BM * C::BN * (int)sizeof(OUT) > C::LDS_BYTES ? 2 : 1, COLS = C::BM / PASSES;
     constexpr int ROW = COLS * (int)sizeof(OUT), PIECES = ROW / 16, EACH = 16 / (int)sizeof(OUT);
-    static_assert(C::BN * ROW <= C::LDS_BYTES && (PASSES == 1 || C::WM == COLS) && PIECES >= 16, "room, and a pass for each row of waves");
+    static_assert(C::BN * ROW <= C::LDS_BYTES && (PASSES == 1 || C::WM == COLS) && PIECES % 8 == 0, "room, and a pass for each row of waves");
+    constexpr int KEYS = PIECES % 16 ? 7 : 15;
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int pass = 0; pass < PASSES; ++pass) {
@@ -580,7 +582,7 @@ __device__ __forceinline__ void leave(const f32x4 (&acc)[C::TI][C::TJ], unsigned
                 for (int i = 0; i < C::TI; ++i) {
                     const int m = C::row0() - pass * COLS + 16 * i + 4 * (lane >> 4);
                     const f32x4 v = acc[i][j] * f;
-                    unsigned char* at = lds + r * ROW + 16 * ((m / EACH) ^ (r & 15));
+                    unsigned char* at = lds + r * ROW + 16 * ((m / EACH) ^ (r & KEYS));
                     if constexpr (sizeof(OUT) == 4) *reinterpret_cast<f32x4*>(at) = v;
                     else *reinterpret_cast<u32x2*>(at + 2 * (m & 4)) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
                 }
@@ -591,7 +593,7 @@ __device__ __forceinline__ void leave(const f32x4 (&acc)[C::TI][C::TJ], unsigned
             const int r = t / PIECES, u = t % PIECES;
             const int64_t n = n0 + r, m = m0 + pass * COLS + u * EACH;
             if (n >= rows || m >= columns) continue;
-            u32x4 v = lds128(lds + r * ROW + 16 * (u ^ (r & 15)));
+            u32x4 v = lds128(lds + r * ROW + 16 * (u ^ (r & KEYS)));
             OUT* to = out + counted.row(n) * ld + m;
             if constexpr (sizeof(OUT) == 4)  // (a sum's rows are whole pieces)
                 if (add) v = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, v) + *reinterpret_cast<const f32x4*>(to));
@@ -704,6 +706,8 @@ using Low32 = NtTile<128, 64, 32, 64, kF32, 3>;
 using Few32 = NtTile<128, 32, 32, 32, kF32, 4>;
 using Big16 = NtTile<256, 256, 128, 64, kF16>;
 using Mid16 = NtTile<128, 128, 64, 64, kF16>;
+using Wide16 = NtTile<192, 256, 96, 64, kF16>;
+using Wide2 = NtTile<192, 256, 96, 64, kF16x2>;
 
 // bytes handed out of a workspace
 struct Area {
@@ -796,26 +800,27 @@ struct FwdArea {
 };
 
 // How a product of m x n numbers over `steps` steps is run, by an estimate of its time in microseconds on 256 CUs: whole rounds of workgroups, one of
-// 256 x 256 a CU or two of 128 x 128, each over a share of the steps, and the shares' sums written and read.  Measured: a step of 256 x 256
-// takes 1.6 us (two planes 2.2), one of 128 x 128 0.9 (1.2) beside another and 0.55 (0.75) alone.
+// 256 x 256 or 192 x 256 a CU or two of 128 x 128, each over a share of the steps, and the shares' sums written and read.  Measured: a step of
+// 256 x 256 takes 1.6 us (two planes 2.2), one of 192 x 256 1.25 (1.7), one of 128 x 128 0.9 (1.2) beside another and 0.55 (0.75) alone.  (dx of 7373 rows of width
+// 768 that count, 50257 entries: 687 us by 192 x 256, 756 by 128 x 128, which leave a third of the CUs' places empty.)
+enum Tile { kMid, kWide, kBig };
 struct Cut {
-    bool big;
+    Tile tile;
     int shares;
     double us;
 };
 Cut cut_for(int64_t m, int64_t n, int steps, bool planes, int pieces_before)
 {
-    Cut best{false, 1, 1e30};
-    for (int big = 0; big < 2; ++big) {
-        const int64_t side = big ? 256 : 128, tiles = ((m + side - 1) / side) * ((n + side - 1) / side);
+    Cut best{kMid, 1, 1e30};
+    for (int tile = kMid; tile <= kBig; ++tile) {
+        const int64_t bm = tile == kMid ? 128 : tile == kWide ? 192 : 256, bn = tile == kMid ? 128 : 256, tiles = ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
         for (int shares = 1; shares <= 32 && shares * 4 <= (steps > 4 ? steps : 4); shares = shares < 4 ? shares + 1 : shares + shares / 2) {
-            const int64_t groups = tiles * shares, slots = big ? 256 : 512;
-            const bool alone = !big && groups <= 256;
-            const double step = (big ? 1.6 : alone ? 0.55 : 0.9) * (planes ? 1.38 : 1.0);
+            const int64_t groups = tiles * shares, slots = tile == kMid ? 512 : 256;
+            const double step = (tile == kBig ? 1.6 : tile == kWide ? 1.25 : groups <= 256 ? 0.55 : 0.9) * (planes ? 1.38 : 1.0);
             const double mb = m * n * 4e-6 * shares;
-            const double us = (double)((groups + slots - 1) / slots) * ((steps + shares - 1) / shares * step + (big ? 4 : 3)) +
+            const double us = (double)((groups + slots - 1) / slots) * ((steps + shares - 1) / shares * step + (tile == kMid ? 3 : 4)) +
                               (shares > 1 || pieces_before ? 3 + 2 * mb / 4 : 0);
-            if (us < best.us && mb < 512) best = Cut{big != 0, shares, us};
+            if (us < best.us && mb < 512) best = Cut{(Tile)tile, shares, us};
         }
     }
     return best;
@@ -966,10 +971,13 @@ int run_product(const Job& j, int shares, hipStream_t st)
                                                                                                 (OUT*)j.out, j.ld, j.part, j.add, j.by);
     return launched();
 }
-template <typename B, typename M, bool DX, typename OUT>
+template <typename B, typename W, typename M, bool DX, typename OUT>
 int product(const Job& j, const Cut& cut, hipStream_t st)
 {
-    if (int rc = cut.big ? run_product<B, DX, OUT>(j, cut.shares, st) : run_product<M, DX, OUT>(j, cut.shares, st)) return rc;
+    const int rc = cut.tile == kBig    ? run_product<B, DX, OUT>(j, cut.shares, st)
+                   : cut.tile == kWide ? run_product<W, DX, OUT>(j, cut.shares, st)
+                                       : run_product<M, DX, OUT>(j, cut.shares, st);
+    if (rc) return rc;
     if (!j.part || !j.last) return 0;
     const int64_t size = j.rows * j.ld, groups = (size + 1023) / 1024;
     xent_shares_kernel<OUT><<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(j.part, cut.shares, j.rows, DX ? j.counted : Counted{}, j.ld, (OUT*)j.out, j.by);
@@ -1048,7 +1056,7 @@ int xent_bwd(const void* x, const void* w, const int64_t* target, const float* l
             // features inside, rows of x outside
             Job j{{a.wt + (size_t)v0 / per * 64, width, a.wt_half * 2}, {a.g, rows, a.g_half * 2}, rows, entries, counted, dx, width, a.dx_part,
                   v0 > 0, last, {a.top + 1, a.dl}};
-            rc = p.f32 ? product<Big2, Mid2, true, float>(j, a.dx_cut, st) : product<Big16, Mid16, true, uint16_t>(j, a.dx_cut, st);
+            rc = p.f32 ? product<Big2, Wide2, Mid2, true, float>(j, a.dx_cut, st) : product<Big16, Wide16, Mid16, true, uint16_t>(j, a.dx_cut, st);
             if (rc) return rc;
         }
         if (dw) {
@@ -1058,10 +1066,10 @@ int xent_bwd(const void* x, const void* w, const int64_t* target, const float* l
             const size_t at = (size_t)v0 * width;
             if (dw_f32) {
                 j.out = (float*)dw + at;
-                rc = p.f32 ? product<Big2, Mid2, false, float>(j, cut, st) : product<Big16, Mid16, false, float>(j, cut, st);
+                rc = p.f32 ? product<Big2, Wide2, Mid2, false, float>(j, cut, st) : product<Big16, Wide16, Mid16, false, float>(j, cut, st);
             } else {
                 j.out = (uint16_t*)dw + at;
-                rc = product<Big16, Mid16, false, uint16_t>(j, cut, st);
+                rc = product<Big16, Wide16, Mid16, false, uint16_t>(j, cut, st);
             }
             if (rc) return rc;
         }

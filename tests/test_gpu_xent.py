@@ -340,3 +340,15 @@ def test_more_rows_than_are_taken_at_once(ops, dtype, rows):
         within(loss, want.loss, want.row_bound, "loss")
         within(dx, want.dx, want.dx_bound, "dx")
         within(dW, want.dW, want.dW_bound, "dW")
+
+
+@pytest.mark.parametrize("shape, dtype", [((3000, 9000, 190), "f32"), ((6000, 9000, 150), "bf16"), ((8000, 9000, 150), "bf16")])
+def test_widths_that_leave_room_in_the_square_tiles(ops, shape, dtype):
+    """dx and dW of some hundred features and many rows: tiles of 192 features, shares of the sums."""
+    x, W, target = inputs(*shape, dtype, ignored=0.2)
+    g = torch.rand((shape[0],), generator=torch.Generator().manual_seed(7)) - 0.3
+    want = Exact(x.cuda(), W.cuda(), target.cuda(), g.cuda(), dtype)
+    loss, _, dx, dW = run(ops[1], x, W, target, g)
+    within(loss, want.loss.cpu(), want.row_bound.cpu(), "loss")
+    within(dx, want.dx.cpu(), want.dx_bound.cpu(), "dx")
+    within(dW, want.dW.cpu(), want.dW_bound.cpu(), "dW")

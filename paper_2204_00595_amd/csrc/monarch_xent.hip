@@ -447,13 +447,21 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2* __restrict_
     const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t >= counted.rows(rows)) return;
     const f32x2* p = part + t * parts;
-    float m = -__builtin_inff();
-    for (int i = lane; i < parts; i += 64) m = fmaxf(m, p[i][0]);
-    m = wave_all(m, max_of);
-    const float base = m == -__builtin_inff() ? 0.f : m;
-    float s = 0.f;
-    for (int i = lane; i < parts; i += 64) s += p[i][1] * exp2_fast(p[i][0] - base);
-    s = wave_all(s, sum_of);
+    f32x2 sum = {-__builtin_inff(), 0.f};
+    for (int i0 = lane; i0 < parts + lane; i0 += 512) {  // (eight loads under way)
+        f32x2 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p[i0 + 64 * i < parts ? i0 + 64 * i : parts - 1];
+        float m = sum[0];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, v[i][0]);
+        const float base = m == -__builtin_inff() ? 0.f : m;
+        float s = sum[1] * exp2_fast(sum[0] - base);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += i0 + 64 * i < parts ? v[i][1] * exp2_fast(v[i][0] - base) : 0.f;
+        sum = f32x2{m, s};
+    }
+    const float m = wave_all(sum[0], max_of), base = m == -__builtin_inff() ? 0.f : m, s = wave_all(sum[1] * exp2_fast(sum[0] - base), sum_of);
     if (lane) return;
     const float all = (base + log2_fast(s)) * kLn2;
     const int64_t row = counted.row(t), at = target[row];

@@ -371,15 +371,11 @@ __device__ __forceinline__ f32x2 joined(f32x2 a, f32x2 b)
     return f32x2{m, a[1] * exp2_fast(a[0] - base) + b[1] * exp2_fast(b[0] - base)};
 }
 
-// Largest (in units of log 2) and sum of the tile's entries for each of its rows of x -> part[t][tile]; the target's logit -> hit[t].
+// Largest (in units of log 2) and sum of the tile's entries for each of its rows of x -> part[t][column]; the target's logit -> hit[t].
 template <typename C, bool TAIL>
-__global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* __restrict__ part, int parts, float* __restrict__ hit)
+__device__ __forceinline__ void part_tile(const Logits& p, int64_t rows, int64_t v0, int64_t t0, unsigned char* lds, f32x2* __restrict__ part, int parts,
+                                          int column, float* __restrict__ hit)
 {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    int tv, tt;
-    const int64_t rows = p.rows();
-    if (!nt_place(blockIdx.x, p.tiles_v, (int)((rows + C::BN - 1) / C::BN), tv, tt)) return;
-    const int64_t v0 = (int64_t)tv * C::BM, t0 = (int64_t)tt * C::BN;
     f32x4 acc[C::TI][C::TJ];
     logits_tile<C, TAIL>(p, rows, v0, t0, lds, acc);
     const int lane = threadIdx.x & 63;
@@ -434,7 +430,26 @@ __global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* 
         f32x2 r = red[c];
 #pragma unroll
         for (int k = 1; k < C::BM / C::WM; ++k) r = joined(r, red[k * C::BN + c]);
-        part[t * parts + tv] = r;
+        part[t * parts + column] = r;
+    }
+}
+
+// `columns` columns of tiles of C, and the rest of the vocabulary by tiles of S, which come last: where tiles of C fill a last round of
+// workgroups less than half, smaller ones in their place end sooner (1024 rows of width 1024, 50257 entries: 788 tiles of 256 x 256 take 116 us,
+// 768 and 80 of 128 x 128 take 104).
+template <typename C, typename S, bool TAIL>
+__global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* __restrict__ part, int parts, int columns, int groups, float* __restrict__ hit)
+{
+    static_assert(S::THREADS == C::THREADS && S::LDS_BYTES <= C::LDS_BYTES, "one launch");
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    int tv, tt;
+    const int64_t rows = p.rows();
+    if (std::is_same_v<C, S> || (int)blockIdx.x < groups) {
+        if (!nt_place(blockIdx.x, columns, (int)((rows + C::BN - 1) / C::BN), tv, tt)) return;
+        part_tile<C, TAIL>(p, rows, (int64_t)tv * C::BM, (int64_t)tt * C::BN, lds, part, parts, tv, hit);
+    } else {
+        if (!nt_place((int)blockIdx.x - groups, parts - columns, (int)((rows + S::BN - 1) / S::BN), tv, tt)) return;
+        part_tile<S, TAIL>(p, rows, (int64_t)columns * C::BM + (int64_t)tv * S::BM, (int64_t)tt * S::BN, lds, part, parts, columns + tv, hit);
     }
 }
 
@@ -706,6 +721,8 @@ using Big = NtTile<256, 256, 128, 64, kBf16>;
 using Mid = NtTile<128, 128, 64, 64, kBf16>;
 using Low = NtTile<128, 64, 32, 64, kBf16>;
 using FewB = NtTile<128, 32, 32, 32, kBf16, 4>;
+using End = NtTile<128, 128, 64, 32, kBf16>;
+using End2 = NtTile<128, 128, 64, 32, kF16x2>;
 using Big2 = NtTile<256, 256, 128, 64, kF16x2>;
 using Mid2 = NtTile<128, 128, 64, 64, kF16x2>;
 using Low2 = NtTile<128, 64, 32, 64, kF16x2>;
@@ -752,6 +769,13 @@ struct Plan {
     int bv() const { return tile() == 0 ? 256 : 128; }
     int bt() const { return tile() == 0 ? 256 : tile() == 1 ? 128 : tile() == 2 ? 64 : 32; }
     int parts() const { return (vocab + bv() - 1) / bv(); }
+    // The forward's tiles of 256 x 256 end with a round that is at most half full: columns before that round, else all.
+    int columns() const
+    {
+        const int64_t all = parts(), across = row_tiles(), whole = all * across / 256 * 256 / across;
+        return tile() == 0 && whole > 0 && (all - whole) * across * 4 <= 256 ? (int)whole : (int)all;
+    }
+    int forward_parts() const { return columns() == parts() ? parts() : columns() + (vocab - columns() * bv() + 127) / 128; }
     int64_t row_tiles() const { return (rows + bt() - 1) / bt(); }
 };
 
@@ -801,7 +825,7 @@ struct FwdArea {
         Area a{base};
         sides.lay(p, a);
         counted.lay(p, a);
-        part = a.take<f32x2>((size_t)p.rows * p.parts());
+        part = a.take<f32x2>((size_t)p.rows * p.forward_parts());
         hit = a.take<float>(p.rows);
         return a.used;
     }
@@ -941,13 +965,16 @@ Logits logits_of(const Plan& p, const Sides& s, const Counted& counted, const vo
 template <typename C>
 int tiles_of(const Logits& l) { return (int)((l.all_rows + C::BN - 1) / C::BN); }
 // Rows that end inside a step have kernels of their own (the test for it in every step costs 14 % of a long product).
-template <typename C, bool TAIL>
-int run_part(const Logits& l, f32x2* part, int parts, float* hit, hipStream_t st)
+template <typename C, bool TAIL = false>
+int run_part(const Plan& p, const Logits& l, const FwdArea& a, hipStream_t st)
 {
     if constexpr (!TAIL && C::KIND != kF16x2)
-        if (l.tail < 8) return run_part<C, true>(l, part, parts, hit, st);
-    if (allow_dynamic_lds((const void*)xent_part_kernel<C, TAIL>, C::LDS_BYTES) != hipSuccess) return -4;
-    xent_part_kernel<C, TAIL><<<nt_grid(l.tiles_v, tiles_of<C>(l)), C::THREADS, C::LDS_BYTES, st>>>(l, part, parts, hit);
+        if (l.tail < 8) return run_part<C, true>(p, l, a, st);
+    using S = std::conditional_t<C::BM == 256, std::conditional_t<C::KIND == kBf16, End, End2>, C>;
+    if (allow_dynamic_lds((const void*)xent_part_kernel<C, S, TAIL>, C::LDS_BYTES) != hipSuccess) return -4;
+    const int columns = p.columns(), parts = p.forward_parts(), groups = nt_grid(columns, tiles_of<C>(l));
+    const int end = parts > columns ? nt_grid(parts - columns, tiles_of<S>(l)) : 0;
+    xent_part_kernel<C, S, TAIL><<<groups + end, C::THREADS, C::LDS_BYTES, st>>>(l, a.part, parts, columns, groups, a.hit);
     return launched();
 }
 template <typename C, bool TAIL>
@@ -1029,12 +1056,11 @@ int xent_fwd(const void* x, const void* w, const int64_t* target, float* loss, f
     int rc = pack_sides(p, a.sides, c, x, w, nullptr, nullptr, st);
     if (rc) return rc;
     const Logits l = logits_of(p, a.sides, counted, x, w, target);
-    const int parts = p.parts();
-    if (p.plain32()) rc = p.rows > 32 ? run_part<Low32, false>(l, a.part, parts, a.hit, st) : run_part<Few32, false>(l, a.part, parts, a.hit, st);
-    else if (p.f32) rc = by_tile<Big2, Mid2, Low2, Few2>(p, [&](auto c) { return run_part<decltype(c), false>(l, a.part, parts, a.hit, st); });
-    else rc = by_tile<Big, Mid, Low, FewB>(p, [&](auto c) { return run_part<decltype(c), false>(l, a.part, parts, a.hit, st); });
+    if (p.plain32()) rc = p.rows > 32 ? run_part<Low32>(p, l, a, st) : run_part<Few32>(p, l, a, st);
+    else if (p.f32) rc = by_tile<Big2, Mid2, Low2, Few2>(p, [&](auto c) { return run_part<decltype(c)>(p, l, a, st); });
+    else rc = by_tile<Big, Mid, Low, FewB>(p, [&](auto c) { return run_part<decltype(c)>(p, l, a, st); });
     if (rc) return rc;
-    xent_join_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a.part, parts, a.hit, target, ignore, vocab, rows, counted, loss, lse);
+    xent_join_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a.part, p.forward_parts(), a.hit, target, ignore, vocab, rows, counted, loss, lse);
     return launched();
 }
 

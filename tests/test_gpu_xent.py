@@ -352,3 +352,16 @@ def test_widths_that_leave_room_in_the_square_tiles(ops, shape, dtype):
     within(loss, want.loss.cpu(), want.row_bound.cpu(), "loss")
     within(dx, want.dx.cpu(), want.dx_bound.cpu(), "dx")
     within(dW, want.dW.cpu(), want.dW_bound.cpu(), "dW")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(300, 33500, 40), (513, 22100, 33)])
+def test_a_vocabulary_that_ends_in_smaller_tiles(ops, shape, dtype):
+    x, W, target = inputs(*shape, dtype, ignored=0.1)
+    target[:40] = shape[1] - 1 - torch.arange(40) * 20
+    want = Exact(x.cuda(), W.cuda(), target.cuda(), torch.ones(shape[0]).cuda(), dtype)
+    counts = target != IGNORE
+    for flags in (0, ops[1].MONARCH_FLAG_SKIP_IGNORED):
+        loss, lse = ops[1].monarch_xent_fwd(x.cuda(), W.cuda(), target.cuda(), flags=flags)
+        within(loss, want.loss.cpu(), want.row_bound.cpu(), "loss")
+        within(lse.cpu()[counts], want.lse.cpu()[counts], want.row_bound.cpu(), "lse")

@@ -3,13 +3,14 @@
 // which moves every singular value s to a s + b s^3 + c s^5 and leaves the singular vectors.  A is taken on the shorter side, r = min(m, n);
 // below X is r x c (the transpose of the block where it is higher than wide).
 //
-// Three products a step (monarch_nt.h): A = X X^T, P = a I + b A + c A A^T (A is symmetric: of the tiles of A and P those on and below the
-// diagonal are computed), X' = P X.  X lies transposed, c rows of r numbers: the first product reads it across, the last along its rows,
-// and writes the next one so.  Operands are binary16 numbers times a power of two, in two planes: entries of X and A are below 2, those
-// of P below |a| + 2 |b| + 4 |c|, and 22 bits of each are kept (five steps of the 3.4445, -4.7750, 2.0315 polynomial lose 2.5e-7 of the
-// result's norm, fp32 products 1e-6 to 2e-6).  bf16 gradients take the same: with one plane (11 bits) the result would be 1.0e-3 to
-// 1.5e-3 off beside its own rounding of 1.7e-3, and far more where a few directions stand out, since small singular values grow up to
-// 485 times and the rounding of the large ones with them.
+// Blocks of up to 64 x 64 are made in one launch, others whose shorter side is at most 192 in two launches a step (both below).  Else three
+// products a step (monarch_nt.h): A = X X^T, P = a I + b A + c A A^T (A is symmetric: of the tiles of A and P those on and below the diagonal
+// are computed), X' = P X.  X lies transposed, c rows of r numbers: the first product reads it across, the last along its rows, and writes
+// the next one so.  Operands are binary16 numbers times a power of two, in two planes: entries of X and A are below 2, those of P below
+// |a| + 2 |b| + 4 |c|, and 22 bits of each are kept (five steps of the 3.4445, -4.7750, 2.0315 polynomial lose 2.5e-7 of the result's norm,
+// fp32 products 1e-6 to 2e-6).  bf16 gradients take the same: with one plane (11 bits) the result would be 1.0e-3 to 1.5e-3 off beside its
+// own rounding of 1.7e-3, and far more where a few directions stand out, since small singular values grow up to 485 times and the
+// rounding of the large ones with them.
 #include "monarch_ortho.h"
 #include "monarch_device.h"
 #include "monarch_nt.h"
@@ -329,6 +330,141 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
     }
 }
 
+// ---- blocks whose shorter side is at most 192: a step in two launches ----
+
+// X' = a X + A (b X + c A X) for 16 rows of X (as it lies: columns of the block's X) a workgroup: each of four waves keeps its rows of A in
+// registers for both products, X and b X + c A X are in LDS (rows of SIDE / 32 steps of 128 bytes, zeros past r, 16-byte piece u of row n in place u ^ (n % 8)).
+// Bound by the latency of a launch and of one load of A (147 KB a workgroup at 192): 16 blocks of 192 x 192 take 8.3 us, where P and the product
+// with it took 4.6 + 4.8 in two launches.  P is never made, which costs r^2 c more products.
+struct Apply {
+    const uint16_t *gram, *x;
+    uint16_t* next;
+    int r, c, blocks, slabs;
+    uint32_t half;
+    float ca, cb, cc;
+};
+
+template <int SIDE, bool LAST, bool TALL, typename T, Out OUT>
+__global__ __launch_bounds__(256) void ortho_apply_kernel(Apply p, Sink sink)
+{
+    constexpr int TILES = SIDE / 64, STEPS = SIDE / 32, ROW = STEPS * 128;
+    __shared__ __attribute__((aligned(128))) unsigned char xs[16 * ROW], zs[16 * ROW];
+    const int total = p.slabs * p.blocks, each = (total + 7) >> 3;  // a block's slabs lie together on an XCD
+    const int t = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= each || t >= total) return;
+    const int block = t / p.slabs, c0 = (t - block * p.slabs) * 16;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r16 = lane & 15, steps = (int)(p.half / 64);
+    const auto row_tile = [&](int i) { return 16 * (wave + 4 * i); };
+    const auto at = [&](int n, int piece) { return n * ROW + 16 * (piece ^ (n & 7)); };
+    const auto number = [&](int n, int m, int plane) { return at(n, (m >> 5) * 8 + plane * 4 + (m >> 3 & 3)) + 2 * (m & 7); };
+    const int pieces = steps * 8;
+    // X, then the wave's rows of A (row tile, step, plane), all under way at once; what is not there reads as zeros
+    u32x4 x[STEPS / 2], a[TILES][STEPS][2];
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr uint32_t kNowhere = 0x7ffffff0u;
+    const int live = p.c - c0 < 16 ? p.c - c0 : 16;
+    const auto rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p.x) + ((int64_t)block * p.c + c0) * p.half, 0, live * (int)p.half * 2, 0x00020000);
+    const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p.gram) + (int64_t)block * p.r * p.half, 0, p.r * (int)p.half * 2, 0x00020000);
+#pragma unroll
+    for (int k = 0; k < STEPS / 2; ++k) {
+        const int u = 16 * k + (tid & 15);
+        x[k] = __builtin_amdgcn_raw_buffer_load_b128(rx, u < pieces ? (tid >> 4) * p.half * 2 + 16 * u : kNowhere, 0, 0);
+    }
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+#pragma unroll
+            for (int plane = 0; plane < 2; ++plane)
+                a[i][s][plane] = __builtin_amdgcn_raw_buffer_load_b128(
+                    ra, s < steps ? (row_tile(i) + r16) * p.half * 2 + 16 * (lane >> 4) + s * 128 + plane * 64 : kNowhere, 0, 0);
+#endif
+#pragma unroll
+    for (int k = 0; k < STEPS / 2; ++k) *reinterpret_cast<u32x4*>(xs + at(tid >> 4, 16 * k + (tid & 15))) = x[k];
+    __syncthreads();
+    f32x4 acc[TILES];
+    // acc[i] = row tile i of A times the rows in `from`; SWAP: its transpose
+    const auto product = [&](const unsigned char* from, auto swap) {
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            f16x8 b[2];
+#pragma unroll
+            for (int plane = 0; plane < 2; ++plane) b[plane] = __builtin_bit_cast(f16x8, lds128(from + at(r16, s * 8 + plane * 4 + (lane >> 4))));
+#pragma unroll
+            for (int k = 0; k < 3; ++k)  // upper x upper, upper x lower, lower x upper
+#pragma unroll
+                for (int i = 0; i < TILES; ++i) {
+                    const f16x8 u = __builtin_bit_cast(f16x8, a[i][s][k == 2]), v = b[k == 1];
+                    acc[i] = decltype(swap)::value ? mfma16(v, u, acc[i]) : mfma16(u, v, acc[i]);
+                }
+        }
+    };
+    const auto x_at = [&](int n, int m) {  // four numbers of X, times kX
+        const u32x2 hi = *reinterpret_cast<const u32x2*>(xs + number(n, m, 0)), lo = *reinterpret_cast<const u32x2*>(xs + number(n, m, 1));
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = f16_value(hi[e >> 1] >> (16 * (e & 1))) + f16_value(lo[e >> 1] >> (16 * (e & 1)));
+        return v;
+    };
+    product(xs, std::false_type{});
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+        const int m = row_tile(i) + 4 * (lane >> 4);
+        // (below 2 |b| + 4 |c|, as P is: times kP; zeros where X has them)
+        const TwoPlanes h = split_planes(x_at(r16, m) * (p.cb * (kP / kX)) + acc[i] * (p.cc * (kP / (kA * kX))));
+#pragma unroll
+        for (int plane = 0; plane < 2; ++plane) *reinterpret_cast<u32x2*>(zs + number(r16, m, plane)) = h.p[plane];
+    }
+    __syncthreads();
+    if constexpr (LAST) {
+        const int tensor = block / sink.blocks;
+        const int64_t at0 = (int64_t)(block - tensor * sink.blocks) * sink.m * sink.n;
+        T* out = (T*)sink.out[tensor] + at0;
+        float* master = OUT == kMasters ? sink.master[tensor] + at0 : nullptr;
+        product(zs, std::bool_constant<!TALL>{});
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            // four numbers that follow one another in the result: of the block's row `row` from `col` on
+            const int four = 4 * (lane >> 4), row = TALL ? c0 + r16 : row_tile(i) + r16, col = TALL ? row_tile(i) + four : c0 + four;
+            if (row >= sink.m || col >= sink.n) continue;
+            f32x4 v;
+            if constexpr (TALL) v = x_at(r16, col);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] = f16_value(*reinterpret_cast<const uint16_t*>(xs + number(four + e, row, 0))) +
+                           f16_value(*reinterpret_cast<const uint16_t*>(xs + number(four + e, row, 1)));
+            v = v * (p.ca / kX) + acc[i] * (1.f / (kA * kP));
+            const int64_t to = (int64_t)row * sink.n + col;
+            if ((sink.n & 3) == 0) {
+                put4<T, OUT>(sink, out + to, OUT == kMasters ? master + to : nullptr, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < sink.n) put<T, OUT>(sink, out + to + e, OUT == kMasters ? master + to + e : nullptr, v[e]);
+            }
+        }
+    } else {
+        product(zs, std::false_type{});
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            const int m = row_tile(i) + 4 * (lane >> 4);
+            const TwoPlanes h = split_planes(x_at(r16, m) * p.ca + acc[i] * (kX / (kA * kP)));
+#pragma unroll
+            for (int plane = 0; plane < 2; ++plane) *reinterpret_cast<u32x2*>(xs + number(r16, m, plane)) = h.p[plane];  // (its lane alone reads it)
+        }
+        __syncthreads();
+        uint16_t* next = p.next + ((int64_t)block * p.c + c0) * p.half;
+#pragma unroll
+        for (int k = 0; k < STEPS / 2; ++k) {
+            const int n = tid >> 4, u = 16 * k + (tid & 15);
+            if (c0 + n < p.c && u < pieces) *reinterpret_cast<u32x4*>(next + (int64_t)n * p.half + 8 * u) = lds128(xs + at(n, u));
+        }
+    }
+}
+
 // ---- small blocks: the whole of it in one launch ----
 
 // A block of up to S x S, zeros around it, in a workgroup of four waves: X both ways round, A and P stay in LDS as operands (rows of S / 32
@@ -536,6 +672,20 @@ int product(const Product& p, const Sink& sink, hipStream_t st)
     return run_product<Low, PART, T, OUT>(p, sink, st);
 }
 
+// Two launches a step instead of three where a launch costs most: up to 512 slabs (two workgroups of four waves for each CU), or blocks near squares, whose
+// P costs as much as the second product with A.  Five steps, two launches a step against three: 16 blocks of 192 x 192 81 against 88 us, 64 of
+// 128 x 128 77 / 89, 128 of 128 x 128 103 / 120, 16 of 192 x 512 (512 slabs) 111 / 120; past the rule, 24 of 192 x 384 (576 slabs) 127 / 115 and
+// 64 of 192 x 768 377 / 254.
+bool by_slabs(const OrthoArea& a, int64_t blocks) { return a.r <= 192 && ((a.c + 15) / 16 * blocks <= 512 || 4 * a.c <= 5 * a.r); }
+template <bool LAST, bool TALL, typename T, Out OUT>
+int run_apply(const Apply& p, const Sink& sink, hipStream_t st)
+{
+    const unsigned grid = (unsigned)((p.slabs * p.blocks + 7) / 8 * 8);
+    if (p.r <= 128) ortho_apply_kernel<128, LAST, TALL, T, OUT><<<grid, 256, 0, st>>>(p, sink);
+    else ortho_apply_kernel<192, LAST, TALL, T, OUT><<<grid, 256, 0, st>>>(p, sink);
+    return launched();
+}
+
 template <typename T, Out OUT>
 int steps_of(const OrthoShape& s, const OrthoSteps& k, OrthoArea& a, const Sink& sink, hipStream_t st)
 {
@@ -555,6 +705,14 @@ int steps_of(const OrthoShape& s, const OrthoSteps& k, OrthoArea& a, const Sink&
         poly.a = poly.b = poly.gram = a.gram;
         poly.rows = a.poly;
         if (int rc = product<kGram, uint16_t, kPlain>(gram, sink, st)) return rc;
+        if (by_slabs(a, p.blocks)) {
+            const Apply apply{a.gram, a.x[i & 1], a.x[(i + 1) & 1], a.r, a.c, p.blocks, (a.c + 15) / 16, a.half, k.a, k.b, k.c};
+            const int rc = i + 1 < k.steps ? run_apply<false, false, uint16_t, kPlain>(apply, sink, st)
+                           : tall          ? run_apply<true, true, T, OUT>(apply, sink, st)
+                                           : run_apply<true, false, T, OUT>(apply, sink, st);
+            if (rc) return rc;
+            continue;
+        }
         if (int rc = product<kPoly, uint16_t, kPlain>(poly, sink, st)) return rc;
         next.a = a.poly;
         next.a_rows = a.r;

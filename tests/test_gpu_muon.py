@@ -214,3 +214,31 @@ def test_refusals(binding):
         binding.monarch_muon_step([G.clone()], [G], [G.clone()], lr=0.1, masters=[G.clone()])   # masters of fp32 weights
     with pytest.raises(TypeError):
         binding.monarch_muon_step(G, [G], [G], lr=0.1)
+
+
+# both sides of the limits of the forms of a step: the shorter side 128 and 192, many slabs of wide and of square blocks
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 128, 129), (1, 129, 131), (2, 192, 192), (1, 193, 193), (40, 66, 210), (30, 330, 100), (70, 100, 110), (2, 200, 260),
+                                   (1, 230, 301), (1, 2000, 65)])
+def test_forms_of_a_step(binding, shape, dtype):
+    G = gradient(shape, dtype)
+    X = binding.monarch_orthogonalize(G.cuda())
+    assert far(X, orthogonal(G)) <= BOUND[dtype]
+    assert torch.equal(X, binding.monarch_orthogonalize(G.cuda()))
+
+
+@pytest.mark.parametrize("masters", [False, True])
+@pytest.mark.parametrize("shape", [(2, 210, 300), (301, 210), (40, 66, 210), (40, 210, 66), (3, 150, 100), (99, 131)])
+def test_muon_step_of_each_form(binding, shape, masters):
+    weight, grad, momentum = gradient(shape, "f32", 100, 0.2), gradient(shape, "f32", 200), gradient(shape, "f32", 300, 5e-3)
+    weight = weight if masters else weight.to(torch.bfloat16).float()
+    update = orthogonal(grad.double() + 0.9 * (0.9 * momentum.double() + grad.double()))
+    scale = max(1.0, shape[-2] / shape[-1]) ** 0.5
+    want = (1 - 0.05 * 0.1) * weight.double() - 0.05 * scale * update
+    w, k = weight.to(torch.bfloat16).cuda(), weight.cuda()
+    binding.monarch_muon_step([w], [grad.cuda()], [momentum.cuda()], lr=0.05, momentum=0.9, weight_decay=0.1, masters=[k] if masters else None)
+    if masters:
+        assert torch.equal(w, k.to(torch.bfloat16))
+    # fp32: the update's share of its bound and one rounding; bf16 weights: 2^-8 and as much of the bound
+    got, bound = (k, BOUND["f32"]) if masters else (w, 2.0 ** -8)
+    assert (got.double().cpu() - want).norm() <= bound * want.norm()

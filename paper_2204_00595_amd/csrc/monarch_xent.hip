@@ -491,8 +491,10 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2* __restrict_
 constexpr float kG = 0x1p14f;  // what exp(l - lse) - [v = target] is stored times
 
 // G of a piece of the vocabulary as an operand of binary16 planes, without the upstream gradient; leaves by way of LDS in runs of 64 bytes and
-// more.  Entries and rows that do not exist are written as zeros.
-template <typename C, bool TAIL>
+// more.  Entries and rows that do not exist are written as zeros.  PAST: G is too long for the caches and leaves them to x and W, which the next
+// tiles read (16384 rows of width 1024, 50257 entries: 1.80 ms for 1.89; 1000 rows of width 256, 20000 entries, whose G stays in them, a
+// training step of 136 us for 131; two planes leave in half lines and take 3 % more either way).
+template <typename C, bool TAIL, bool PAST>
 __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const float* __restrict__ lse, uint16_t* __restrict__ g, uint32_t g_half)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
@@ -548,7 +550,9 @@ __global__ __launch_bounds__(C::THREADS) void xent_grad_kernel(Logits p, const f
             const int r = at / (C::BM / 8), u = at % (C::BM / 8);
             const int64_t k = (int64_t)tv * C::BM + 8 * u;
             uint16_t* to = g + (t0 + r) * (int64_t)g_half + (C::PL == 1 ? k : (k >> 5) * 64 + 32 * plane + (k & 31));
-            *reinterpret_cast<u32x4*>(to) = lds128(lds + r * (2 * C::BM) + 16 * (u ^ (r & 15)));
+            const u32x4 v = lds128(lds + r * (2 * C::BM) + 16 * (u ^ (r & 15)));
+            if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(to));
+            else *reinterpret_cast<u32x4*>(to) = v;
         }
     }
 }
@@ -832,9 +836,11 @@ struct FwdArea {
 };
 
 // How a product of m x n numbers over `steps` steps is run, by an estimate of its time in microseconds on 256 CUs: whole rounds of workgroups, one of
-// 256 x 256 or 192 x 256 a CU or two of 128 x 128, each over a share of the steps, and the shares' sums written and read.  Measured: a step of
-// 256 x 256 takes 1.6 us (two planes 2.2), one of 192 x 256 1.25 (1.7), one of 128 x 128 0.9 (1.2) beside another and 0.55 (0.75) alone.  (dx of 7373 rows of width
-// 768 that count, 50257 entries: 687 us by 192 x 256, 756 by 128 x 128, which leave a third of the CUs' places empty.)
+// 256 x 256 or 192 x 256 a CU or two of 128 x 128, each over a share of the steps, and the shares' sums written and read.  Measured where the clock
+// is not held down by power: a step of 256 x 256 takes 1.6 us (two planes 2.2), one of 192 x 256 1.25 (1.7), one of 128 x 128 0.9 (1.2) beside
+// another and 0.55 (0.75) alone.  (On all CUs at once for long they take up to a fifth more, all alike; with 1.9, 1.45 and 0.94 for them the
+// choices are worse: 16384 rows of width 1024 6.83 ms for 6.03.  dx of 7373 rows of width 768 that count, 50257 entries: 687 us by
+// 192 x 256, 756 by 128 x 128, which leave a third of the CUs' places empty.)
 enum Tile { kMid, kWide, kBig };
 struct Cut {
     Tile tile;
@@ -858,7 +864,9 @@ Cut cut_for(int64_t m, int64_t n, int steps, bool planes, int pieces_before)
     return best;
 }
 
-constexpr size_t kPieceBytes = (size_t)1 << 29;  // G of a piece of the vocabulary, where the workspace has room for it
+// G of a piece of the vocabulary at most, where the workspace has room for it.  (G that fits the 256 MB cache is no gain: pieces of 160 MB take 4 to 15 %
+// longer than pieces of 512 MB or 1 GB, since each fills whole rounds of workgroups worse.)
+constexpr size_t kPieceBytes = (size_t)1 << 30;
 
 struct BwdArea {
     Sides sides;
@@ -868,6 +876,8 @@ struct BwdArea {
     int piece;                                   // entries of the vocabulary, whole tiles
     Cut dx_cut, dw_cut, dw_last;                 // of a whole piece, and of the last one
     uint32_t g_half, wt_half, xt_half;
+    double us;                                   // estimate of all products with G
+    bool past;                                   // G does not fit the 256 MB cache
     int entries_of(const Plan& p, int v0) const { return p.vocab - v0 < piece ? p.vocab - v0 : piece; }
     size_t lay(const Plan& p, char* base, int64_t tiles_of_piece)
     {
@@ -882,7 +892,10 @@ struct BwdArea {
         dx_cut = cut_for(p.width, p.rows, (first + per - 1) / per, p.f32, several);
         dw_cut = cut_for(p.width, first, (int)((p.rows + per - 1) / per), p.f32, 0);
         dw_last = cut_for(p.width, last, (int)((p.rows + per - 1) / per), p.f32, 0);
+        // (20 us: a piece's launches, and its last round of tiles of G)
+        us = (p.vocab - last) / piece * (dx_cut.us + dw_cut.us + 20) + dx_cut.us * last / first + dw_last.us;
         g_half = p.half(piece);
+        past = (size_t)tokens * g_half * 2 > (size_t)1 << 28;
         wt_half = p.half((int64_t)p.parts() * p.bv());
         xt_half = p.half(tokens);
         wt = a.take<uint16_t>((size_t)p.width * wt_half);
@@ -896,17 +909,23 @@ struct BwdArea {
         dw_part = one || two ? a.take<float>((one > two ? one : two) * sum_ld(p.width)) : nullptr;
         return a.used;
     }
-    // Pieces as long as kPieceBytes and a workspace of `room` bytes allow, a little shorter where the tiles of dW then fill whole rounds; 0: not even
-    // one tile of the vocabulary fits.
+    // Pieces as long as kPieceBytes and a workspace of `room` bytes allow, or as many tiles as fill whole rounds of dW's, whichever is estimated to end
+    // sooner; 0: not even one tile of the vocabulary fits.
     size_t fit(const Plan& p, char* base, size_t room)
     {
         const int64_t tiles = p.parts(), tokens = p.row_tiles() * p.bt(), across = (p.width + 255) / 256, round = 256 / across * (256 / p.bv());
         int64_t most = (int64_t)(kPieceBytes / ((size_t)tokens * (p.f32 ? 4 : 2))) / p.bv();
         most = most < 1 ? 1 : most > tiles ? tiles : most;
         for (; most > 0; most = most > 16 ? most - most / 8 : most - 1) {
-            const int64_t each = most < tiles && round > 0 && most >= round ? most / round * round : most;
-            const size_t need = lay(p, base, each);
-            if (need <= room) return need;
+            if (lay(p, base, most) > room) continue;
+            int64_t best = most;
+            double least = us * 0.98;  // (a difference below that is none)
+            for (int64_t each = round; round > 0 && each < most; each += round)
+                if (lay(p, base, each) <= room && us < least) {
+                    best = each;
+                    least = us;
+                }
+            return lay(p, base, best);
         }
         return 0;
     }
@@ -977,13 +996,15 @@ int run_part(const Plan& p, const Logits& l, const FwdArea& a, hipStream_t st)
     xent_part_kernel<C, S, TAIL><<<groups + end, C::THREADS, C::LDS_BYTES, st>>>(l, a.part, parts, columns, groups, a.hit);
     return launched();
 }
-template <typename C, bool TAIL>
+template <typename C, bool TAIL = false, bool PAST = false>
 int run_grad(const Logits& l, const BwdArea& a, hipStream_t st)
 {
     if constexpr (!TAIL && C::KIND != kF16x2)
-        if (l.tail < 8) return run_grad<C, true>(l, a, st);
-    if (allow_dynamic_lds((const void*)xent_grad_kernel<C, TAIL>, C::LDS_BYTES) != hipSuccess) return -4;
-    xent_grad_kernel<C, TAIL><<<nt_grid(l.tiles_v, tiles_of<C>(l)), C::THREADS, C::LDS_BYTES, st>>>(l, a.lse, a.g, a.g_half);
+        if (l.tail < 8) return run_grad<C, true, PAST>(l, a, st);
+    if constexpr (!PAST && C::BM == 256 && C::PL == 1)
+        if (a.past) return run_grad<C, TAIL, true>(l, a, st);
+    if (allow_dynamic_lds((const void*)xent_grad_kernel<C, TAIL, PAST>, C::LDS_BYTES) != hipSuccess) return -4;
+    xent_grad_kernel<C, TAIL, PAST><<<nt_grid(l.tiles_v, tiles_of<C>(l)), C::THREADS, C::LDS_BYTES, st>>>(l, a.lse, a.g, a.g_half);
     return launched();
 }
 
@@ -1083,8 +1104,8 @@ int xent_bwd(const void* x, const void* w, const int64_t* target, const float* l
         const bool last = v0 + a.piece >= vocab;
         l.v0 = v0;
         l.tiles_v = (entries + p.bv() - 1) / p.bv();
-        if (p.f32) rc = by_tile<Big2, Mid2, Low2, Low2>(p, [&](auto c) { return run_grad<decltype(c), false>(l, a, st); });
-        else rc = by_tile<Big, Mid, Low, Low>(p, [&](auto c) { return run_grad<decltype(c), false>(l, a, st); });
+        if (p.f32) rc = by_tile<Big2, Mid2, Low2, Low2>(p, [&](auto c) { return run_grad<decltype(c)>(l, a, st); });
+        else rc = by_tile<Big, Mid, Low, Low>(p, [&](auto c) { return run_grad<decltype(c)>(l, a, st); });
         if (rc) return rc;
         if (dx) {
             // features inside, rows of x outside

@@ -23,20 +23,23 @@ struct NtOperand {
 
 enum NtKind { kBf16, kF16, kF16x2, kF32 };
 
-// A workgroup's BM x BN tile, a wave's WM x WN part of it.
-template <int BM_, int BN_, int WM_, int WN_, NtKind KIND_, int RING_ = 2, int SUB_ = 1>
+// A workgroup's BM x BN tile, a wave's WM x WN part of it.  SPLIT: the steps that come together go to as many groups of waves, whose sums nt_product adds
+// up at its end; group 0 has them.
+template <int BM_, int BN_, int WM_, int WN_, NtKind KIND_, int RING_ = 2, int SUB_ = 1, bool SPLIT_ = false>
 struct NtTile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, RING = RING_;
     static constexpr int SUB = SUB_;  // steps that come together, between two barriers; RING times as many are in LDS
     static constexpr NtKind KIND = KIND_;
     static constexpr int PL = KIND == kF16x2 ? 2 : 1;  // planes
-    static constexpr int WAVES = (BM / WM) * (BN / WN), THREADS = 64 * WAVES;
+    static constexpr int GROUPS = SPLIT_ ? SUB : 1;
+    static constexpr int WAVES = (BM / WM) * (BN / WN), THREADS = 64 * WAVES * GROUPS;  // waves of a group
     static constexpr int TI = WM / 16, TJ = WN / 16;
     static constexpr int BUFFER = SUB * (BM + BN) * 128, LDS_BYTES = RING * BUFFER;
     static constexpr int ASK_A = BM / 8 / WAVES, ASK_B = BN / 8 / WAVES;  // requests of a wave per step, 8 rows each
     static_assert(RING >= 2 && RING <= 4, "ring");
     static_assert(ASK_A * 8 * WAVES == BM && ASK_B * 8 * WAVES == BN, "whole requests");
-    static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
+    static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) % WAVES; }
+    static __device__ __forceinline__ int group() { return GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / WAVES; }
     static __device__ __forceinline__ int row0() { return wave() / (BN / WN) * WM; }  // of the wave's part
     static __device__ __forceinline__ int col0() { return wave() % (BN / WN) * WN; }
 };
@@ -156,10 +159,12 @@ __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const
     const SideB side_b(B, b0, wave, lane);
     auto to = (__attribute__((address_space(3))) unsigned char*)lds + wave * 1024;
     const int groups = (steps + C::SUB - 1) / C::SUB;
+    constexpr int EACH = C::SUB / C::GROUPS;  // of the steps that come together, this wave's
+    const int mine = C::group();
     auto ask = [&](int group, int buffer) {
 #pragma unroll
-        for (int u = 0; u < C::SUB; ++u) {
-            const int step = group * C::SUB + u;
+        for (int i = 0; i < EACH; ++i) {
+            const int u = i + mine, step = group * C::SUB + u;
             const bool live = C::SUB == 1 || step < steps;  // (past the end: zeros)
             side_a.ask(step0 + step, live, to + buffer * C::BUFFER + u * (C::BM + C::BN) * 128);
             side_b.ask(step0 + step, live, to + buffer * C::BUFFER + (u * (C::BM + C::BN) + C::BM) * 128);
@@ -227,7 +232,7 @@ __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const
             }
         }
     };
-    constexpr int PENDING = C::SUB * (C::ASK_A + C::ASK_B);
+    constexpr int PENDING = EACH * (C::ASK_A + C::ASK_B);
     for (int s = 0; s < C::RING - 1 && s < groups; ++s) ask(s, s);
     int buffer = 0;
     for (int s = 0; s < groups; ++s) {
@@ -239,8 +244,8 @@ __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const
         asm volatile("" ::: "memory");
         if (s + C::RING - 1 < groups) ask(s + C::RING - 1, buffer ? buffer - 1 : C::RING - 1);
 #pragma unroll
-        for (int u = 0; u < C::SUB; ++u) {
-            const int step = s * C::SUB + u, offset = buffer * C::BUFFER + u * (C::BM + C::BN) * 128;
+        for (int i = 0; i < EACH; ++i) {
+            const int u = i + mine, step = s * C::SUB + u, offset = buffer * C::BUFFER + u * (C::BM + C::BN) * 128;
             if constexpr (TAIL) {
                 if (step + 1 == steps && tail < 8) {
                     products(std::true_type{}, offset);
@@ -250,6 +255,26 @@ __device__ __forceinline__ void nt_product(const NtOperand& A, int64_t a0, const
             products(std::false_type{}, offset);
         }
         buffer = buffer + 1 == C::RING ? 0 : buffer + 1;
+    }
+    if constexpr (C::GROUPS > 1) {
+        static_assert((C::GROUPS - 1) * C::BM * C::BN * 4 <= C::LDS_BYTES, "room for the other groups' sums");
+        const auto at = [&](int group, int i, int j) {
+            return reinterpret_cast<f32x4*>(lds + (group - 1) * C::BM * C::BN * 4 + ((wave * C::TI + i) * C::TJ + j) * 1024 + lane * 16);
+        };
+        __syncthreads();
+        if (mine)
+#pragma unroll
+            for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+                for (int j = 0; j < C::TJ; ++j) *at(mine, i, j) = acc[i][j];
+        __syncthreads();
+        if (!mine)
+#pragma unroll
+            for (int g = 1; g < C::GROUPS; ++g)
+#pragma unroll
+                for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+                    for (int j = 0; j < C::TJ; ++j) acc[i][j] += *at(g, i, j);
     }
 #endif
 }

@@ -232,7 +232,7 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
                 for (int plane = 0; plane < 2; ++plane) {
                     const int m = m0 + 16 * i, n = n0 + 16 * j;
                     gram[i][j][plane] = u32x2{0, 0};
-                    if (n < p.b_rows && (uint32_t)m * 2 < p.rows_half)
+                    if (!C::group() && n < p.b_rows && (uint32_t)m * 2 < p.rows_half)
                         gram[i][j][plane] = *reinterpret_cast<const u32x2*>(p.gram + ((int64_t)block * p.b_rows + n) * p.rows_half + place(m, plane));
                 }
     }
@@ -253,8 +253,9 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
     const int mw = C::row0() + 4 * (lane >> 4), nw = C::col0() + (lane & 15);  // m0, n0 in the tile
     TwoPlanes h[C::TI][C::TJ];
     __syncthreads();
+    if (!C::group())
 #pragma unroll
-    for (int j = 0; j < C::TJ; ++j)
+      for (int j = 0; j < C::TJ; ++j)
 #pragma unroll
         for (int i = 0; i < C::TI; ++i) {
             f32x4 v = acc[i][j];
@@ -315,8 +316,9 @@ __global__ __launch_bounds__(C::THREADS) void ortho_product_kernel(Product p, Si
         leave(tb * C::BN, p.b_rows, ta * C::BM);
         if (HALF && ta != tb) {  // the other side of the diagonal
             __syncthreads();
+            if (!C::group())
 #pragma unroll
-            for (int j = 0; j < C::TJ; ++j)
+              for (int j = 0; j < C::TJ; ++j)
 #pragma unroll
                 for (int i = 0; i < C::TI; ++i) {
                     const int r = mw + 16 * i + (lane & 3), k = (nw & ~3) + 16 * j;
@@ -657,19 +659,25 @@ int run_product(Product p, const Sink& sink, hipStream_t st)
     ortho_product_kernel<C, PART, T, OUT><<<grid, C::THREADS, C::LDS_BYTES, st>>>(p, sink);
     return launched();
 }
+// The largest tile of which there is one for each CU.  Measured, five steps: 8 blocks of 150 x 333 109 us by 64 x 64, 76 by 32 x 32; 48 of 1024 x 256 407 us
+// all by 128 x 128, 393 by the rule.  Tiles of 64 have two groups of waves each (A of those 48: 23 us, 26 by one group), those of 32 four where
+// there are at most 256 (2 blocks of 180 x 4000 209 us for 299, 8 of 150 x 333 74 for 81), one where there are more (A of 16 blocks of
+// 192 x 192: 5.0 us, 5.7 by two groups).
 template <Part PART, typename T, Out OUT>
 int product(const Product& p, const Sink& sink, hipStream_t st)
 {
     using Big = NtTile<128, 128, 64, 64, kF16x2>;
-    using Mid = NtTile<64, 64, 32, 32, kF16x2, 2, 2>;
+    using Mid = NtTile<64, 64, 32, 32, kF16x2, 2, 2, true>;
     using Low = NtTile<32, 32, 16, 16, kF16x2, 2, 2>;
+    using Lone = NtTile<32, 32, 16, 16, kF16x2, 2, 4, true>;
     const auto tiles = [&](int side) {
         const int64_t a = (p.a_rows + side - 1) / side, b = (p.b_rows + side - 1) / side;
         return (PART == kGram || PART == kPoly ? a * (a + 1) / 2 : a * b) * p.blocks;
     };
     if (tiles(128) >= 256) return run_product<Big, PART, T, OUT>(p, sink, st);
     if (tiles(64) >= 256) return run_product<Mid, PART, T, OUT>(p, sink, st);
-    return run_product<Low, PART, T, OUT>(p, sink, st);
+    if (tiles(32) > 256) return run_product<Low, PART, T, OUT>(p, sink, st);
+    return run_product<Lone, PART, T, OUT>(p, sink, st);
 }
 
 // Two launches a step instead of three where a launch costs most: up to 512 slabs (two workgroups of four waves for each CU), or blocks near squares, whose

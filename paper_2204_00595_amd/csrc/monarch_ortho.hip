@@ -666,7 +666,9 @@ int run_product(Product p, const Sink& sink, hipStream_t st)
 template <Part PART, typename T, Out OUT>
 int product(const Product& p, const Sink& sink, hipStream_t st)
 {
-    using Big = NtTile<128, 128, 64, 64, kF16x2>;
+    // (eight waves; four take 6 % longer on a block of 4096 x 4096.  The last product reads and writes weights and masters: 51 us with four waves,
+    // 43 with eight, 40 with sixteen for those 48 blocks)
+    using Big = NtTile<128, 128, PART == kLast ? 32 : 64, 32, kF16x2>;
     using Mid = NtTile<64, 64, 32, 32, kF16x2, 2, 2, true>;
     using Low = NtTile<32, 32, 16, 16, kF16x2, 2, 2>;
     using Lone = NtTile<32, 32, 16, 16, kF16x2, 2, 4, true>;

@@ -369,9 +369,9 @@ size_t monarch_xent_fwd_workspace_bytes(int64_t rows, int vocab, int width, mona
  * g[t] = dloss[t * dloss_stride] / *divisor (fp32 on the device; stride 0: one value for all rows; divisor NULL: 1), 0 for
  * ignored rows, whose x has no influence on dW whatever it holds.  dx (rows, width) and dW (vocab, width) of `dtype` (dW fp32
  * with MONARCH_FLAG_WGRAD_F32) are overwritten; either may be NULL.  The logits are computed a second time, a piece of the
- * vocabulary after the other; in the bf16 path G is rounded to bf16.  `workspace`: the call runs best with
- * monarch_xent_bwd_workspace_bytes(...) bytes and takes less, down to room for G of 256 entries of the vocabulary (in more pieces; in the
- * bf16 path dx is then added up in fp32 there), below which it returns MONARCH_ERR_WORKSPACE. */
+ * vocabulary after the other; G is held with 11 bits of each number in the bf16 path and 22 in the fp32 path.  `workspace`: the call runs best
+ * with monarch_xent_bwd_workspace_bytes(...) bytes and takes less, down to room for G of 256 entries of the vocabulary (in more pieces, between
+ * which dx is added up in fp32), below which it returns MONARCH_ERR_WORKSPACE.  Sums are made in a fixed order (bit-reproducible). */
 int monarch_xent_bwd(const void* x, const void* W, const int64_t* target, const float* lse,
                      const float* dloss, int64_t dloss_stride, const float* divisor, void* dx, void* dW,
                      int64_t rows, int vocab, int width, int64_t ignore_index,

@@ -71,7 +71,9 @@ struct Counted {
     __device__ __forceinline__ int64_t row(int64_t i) const { return at ? at[i] : i; }
 };
 
-constexpr int kTops = 1024;  // workgroups, at most, that leave the largest magnitude they met
+constexpr int kTops = 1024;    // workgroups, at most, that leave the largest magnitude they met
+template <typename T>
+constexpr int kRowWaves = sizeof(T) == 2 ? 8 : 4;  // waves of those, a row each at a time (fp32 rows, read twice, 64 us for 50257 x 768; 74 with eight)
 
 // Largest finite magnitude of `n` values (a workgroup of 256).
 __device__ __forceinline__ float largest_of(const float* __restrict__ v, int n)
@@ -105,16 +107,23 @@ __device__ __forceinline__ float take_row(const T* __restrict__ s, int width, ui
     const int lane = threadIdx.x & 63;
     float m = 0.f;
     if constexpr (sizeof(T) == 2) {
-        for (int k = lane * 8; k < width; k += 512) {
-            const u32x4 u = eight_of(s, k, width);
-            uint32_t t = 0;  // (magnitudes of bf16 numbers are in the order of their bits)
+        uint32_t t = 0;  // (magnitudes of bf16 numbers are in the order of their bits)
+        const int end = d ? (int)row_half : width;
+        for (int k0 = lane * 8; k0 < end; k0 += 1024) {  // (two loads under way)
+            u32x4 u[2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t h = (u[e >> 1] >> (16 * (e & 1))) & 0x7fffu;
-                t = h < 0x7f80u && h > t ? h : t;
+            for (int i = 0; i < 2; ++i) u[i] = eight_of(s, k0 + 512 * i, width);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t h = (u[i][e >> 1] >> (16 * (e & 1))) & 0x7fffu;
+                    t = h < 0x7f80u && h > t ? h : t;
+                }
+                if (d && k0 + 512 * i < end) *reinterpret_cast<u32x4*>(d + k0 + 512 * i) = u[i];
             }
-            m = fmaxf(m, __uint_as_float(t << 16));
         }
+        m = __uint_as_float(t << 16);
     } else {
         const int quads = (width & 3) == 0 ? width / 4 : 0;
         for (int k0 = lane; k0 < quads + lane; k0 += 256) {  // (four loads under way; past the end the last quad once more)
@@ -129,10 +138,8 @@ __device__ __forceinline__ float take_row(const T* __restrict__ s, int width, ui
         for (int k = 4 * quads + lane; k < width; k += 64) m = fmaxf(m, finite_magnitude(s[k]));
     }
     m = wave_all(m, max_of);
-    if (!d) return m;
-    if constexpr (sizeof(T) == 2) {
-        for (uint32_t k = lane * 8; k < row_half; k += 512) *reinterpret_cast<u32x4*>(d + k) = eight_of(s, k, width);
-    } else {
+    if constexpr (sizeof(T) == 4) {
+        if (!d) return m;
         const float up = scale_for(m);
         if (lane == 0) *inv = inverse_power(up);
         for (uint32_t k = lane * 8; k < row_half / 2; k += 512) {
@@ -176,14 +183,14 @@ struct Counting {  // the rows of x that count; what is kept of them
 // itself which of those before them count, so that no launch comes before this one (as launches of their own, three for a forward and three
 // for a backward of 777 rows of width 330, 8191 entries: 10 us more).  `zero` (may be null): the rows of dx that do not count become zero.
 template <typename T>
-__global__ __launch_bounds__(256) void xent_rows_kernel(Taken<T> x, Counting c, Taken<T> w, int width, uint32_t row_half, T* __restrict__ zero)
+__global__ __launch_bounds__(64 * kRowWaves<T>) void xent_rows_kernel(Taken<T> x, Counting c, Taken<T> w, int width, uint32_t row_half, T* __restrict__ zero)
 {
-    __shared__ float top_of[4];
-    __shared__ int count_of[4];
+    __shared__ float top_of[kRowWaves<T>];
+    __shared__ int count_of[kRowWaves<T>];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = (int)blockIdx.x - x.groups;
     float all = 0.f;
     if (group >= 0) {
-        for (int64_t row = (int64_t)group * 4 + wave; row < w.rows; row += (int64_t)w.groups * 4)
+        for (int64_t row = (int64_t)group * kRowWaves<T> + wave; row < w.rows; row += (int64_t)w.groups * kRowWaves<T>)
             all = fmaxf(all, take_row(w.src + row * width, width, w.dst ? w.dst + row * (int64_t)row_half : nullptr, row_half, w.inv + row));
     } else {
         const int64_t each = (x.rows + x.groups - 1) / x.groups, i = blockIdx.x * each, i0 = i < x.rows ? i : x.rows;
@@ -192,18 +199,20 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(Taken<T> x, Counting c, 
         if (c.at) {
             int before = 0;
 #pragma unroll 8
-            for (int64_t k = threadIdx.x; k < i0; k += 256) before += c.target[k] != c.ignore;
+            for (int64_t k = threadIdx.x; k < i0; k += 64 * kRowWaves<T>) before += c.target[k] != c.ignore;
 #pragma unroll
             for (int d = 32; d > 0; d >>= 1) before += __shfl_xor(before, d);
             if (lane == 0) count_of[wave] = before;
             __syncthreads();
-            place = count_of[0] + count_of[1] + count_of[2] + count_of[3];
+            place = 0;
+#pragma unroll
+            for (int i = 0; i < kRowWaves<T>; ++i) place += count_of[i];
         }
         const float by = c.dl && c.divisor ? 1.f / *c.divisor : 1.f;
         for (int64_t b = i0; b < i1; b += 64) {
             const int64_t t = b + lane < i1 ? c.target[b + lane] : c.ignore;
             const uint64_t counts = c.at ? __ballot(t != c.ignore) : ~(uint64_t)0;
-            for (int r = wave; r < 64 && b + r < i1; r += 4) {
+            for (int r = wave; r < 64 && b + r < i1; r += kRowWaves<T>) {
                 const int64_t from = b + r;
                 if (!(counts >> r & 1)) {
                     if (zero)
@@ -237,7 +246,10 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(Taken<T> x, Counting c, 
     if (!tops) return;
     if (lane == 0) top_of[wave] = all;
     __syncthreads();
-    if (threadIdx.x == 0) tops[group >= 0 ? group : (int)blockIdx.x] = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
+    if (threadIdx.x) return;
+#pragma unroll
+    for (int i = 1; i < kRowWaves<T>; ++i) all = fmaxf(all, top_of[i]);
+    tops[group >= 0 ? group : (int)blockIdx.x] = all;
 }
 
 // Columns of src (rows x width) as rows of an operand of binary16 planes, 64 x 64 at a time, times the power of two for the largest of
@@ -638,10 +650,21 @@ __global__ __launch_bounds__(C::THREADS) void xent_product_kernel(NtOperand am, 
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int tm, tn;
-    // (the shares of a tile follow one another on other XCDs; those of neighbouring tiles lie together)
-    const int tiles8 = (int)gridDim.x / shares, share = (int)blockIdx.x / tiles8;
     const int64_t rows = DX ? counted.rows(all_rows) : all_rows;
-    if (!nt_place((int)blockIdx.x - share * tiles8, tiles_m, (int)((rows + C::BN - 1) / C::BN), tm, tn)) return;
+    const int tiles_n = (int)((rows + C::BN - 1) / C::BN), all = (int)gridDim.x / shares;
+    int share;
+    if (shares % 8 == 0) {
+        // a share's tiles lie together on an XCD, whose L2 then reads its part of both operands once
+        const int at = (int)blockIdx.x >> 3;
+        share = at / all * 8 + (int)(blockIdx.x & 7);
+        tm = at % all % tiles_m;
+        tn = at % all / tiles_m;
+        if (tn >= tiles_n) return;
+    } else {
+        // the shares of a tile follow one another on other XCDs; those of neighbouring tiles lie together
+        share = (int)blockIdx.x / all;
+        if (!nt_place((int)blockIdx.x - share * all, tiles_m, tiles_n, tm, tn)) return;
+    }
     constexpr int STEP = C::PL == 2 ? 32 : 64;
     const int steps = (int)(((DX ? depth : counted.rows(depth)) + STEP - 1) / STEP);
     const int each = (steps + shares - 1) / shares, first = share * each, count = steps - first < each ? steps - first : each;
@@ -840,7 +863,9 @@ struct FwdArea {
 // is not held down by power: a step of 256 x 256 takes 1.6 us (two planes 2.2), one of 192 x 256 1.25 (1.7), one of 128 x 128 0.9 (1.2) beside
 // another and 0.55 (0.75) alone.  (On all CUs at once for long they take up to a fifth more, all alike; with 1.9, 1.45 and 0.94 for them the
 // choices are worse: 16384 rows of width 1024 6.83 ms for 6.03.  dx of 7373 rows of width 768 that count, 50257 entries: 687 us by
-// 192 x 256, 756 by 128 x 128, which leave a third of the CUs' places empty.)
+// 192 x 256, 756 by 128 x 128, which leave a third of the CUs' places empty.)  Shares in eights are spread over the XCDs, a share's tiles on one of
+// them, whose L2 reads its part of the operands once; few tiles in other numbers of shares are bound by what their tiles read (dx of 300
+// rows of width 768: 74 us in 28 shares, 32 in 24).
 enum Tile { kMid, kWide, kBig };
 struct Cut {
     Tile tile;
@@ -852,12 +877,14 @@ Cut cut_for(int64_t m, int64_t n, int steps, bool planes, int pieces_before)
     Cut best{kMid, 1, 1e30};
     for (int tile = kMid; tile <= kBig; ++tile) {
         const int64_t bm = tile == kMid ? 128 : tile == kWide ? 192 : 256, bn = tile == kMid ? 128 : 256, tiles = ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
-        for (int shares = 1; shares <= 32 && shares * 4 <= (steps > 4 ? steps : 4); shares = shares < 4 ? shares + 1 : shares + shares / 2) {
+        for (int shares = 1; shares <= 32 && shares * 4 <= (steps > 4 ? steps : 4); shares = shares < 6 ? shares + 1 : shares < 12 ? shares + 2 : shares + 4) {
             const int64_t groups = tiles * shares, slots = tile == kMid ? 512 : 256;
             const double step = (tile == kBig ? 1.6 : tile == kWide ? 1.25 : groups <= 256 ? 0.55 : 0.9) * (planes ? 1.38 : 1.0);
             const double mb = m * n * 4e-6 * shares;
-            const double us = (double)((groups + slots - 1) / slots) * ((steps + shares - 1) / shares * step + (tile == kMid ? 3 : 4)) +
-                              (shares > 1 || pieces_before ? 3 + 2 * mb / 4 : 0);
+            double us = (double)((groups + slots - 1) / slots) * ((steps + shares - 1) / shares * step + (tile == kMid ? 3 : 4));
+            const double reads = tiles * steps * (bm + bn) * 128e-6 / 6.5;  // where the tiles that read the same lie on different XCDs
+            if (shares > 1 && shares % 8 && tiles < 64 && us < reads) us = reads;
+            if (shares > 1 || pieces_before) us += 3 + 2 * mb / 4;
             if (us < best.us && mb < 512) best = Cut{(Tile)tile, shares, us};
         }
     }
@@ -933,15 +960,20 @@ struct BwdArea {
 
 int launched() { return hip_status(hipGetLastError()); }
 
-int rows_grid(int64_t rows) { return (int)((rows + 3) / 4 < kTops ? (rows + 3) / 4 : kTops); }
+template <typename T>
+int rows_grid(int64_t rows)
+{
+    const int64_t all = (rows + kRowWaves<T> - 1) / kRowWaves<T>;
+    return (int)(all < kTops ? all : kTops);
+}
 // Which rows count, rows of x and W as operands where they do not serve as they are, and (tops) the largest magnitudes.
 template <typename T>
 int run_rows(const Plan& p, const Sides& s, const Counting& c, const void* x, const void* w, float* tops, void* dx, hipStream_t st)
 {
-    const Taken<T> tx{(const T*)x, p.rows, s.x, s.xinv, tops, p.packs_x() || tops ? rows_grid(p.rows) : 0};
-    const Taken<T> tw{(const T*)w, p.vocab, s.w, s.winv, tops ? tops + kTops : nullptr, p.packs() || tops ? rows_grid(p.vocab) : 0};
+    const Taken<T> tx{(const T*)x, p.rows, s.x, s.xinv, tops, p.packs_x() || tops ? rows_grid<T>(p.rows) : 0};
+    const Taken<T> tw{(const T*)w, p.vocab, s.w, s.winv, tops ? tops + kTops : nullptr, p.packs() || tops ? rows_grid<T>(p.vocab) : 0};
     if (!(tx.groups + tw.groups)) return 0;
-    xent_rows_kernel<T><<<tx.groups + tw.groups, 256, 0, st>>>(tx, c, tw, p.width, p.half(p.width), (T*)dx);
+    xent_rows_kernel<T><<<tx.groups + tw.groups, 64 * kRowWaves<T>, 0, st>>>(tx, c, tw, p.width, p.half(p.width), (T*)dx);
     return launched();
 }
 int pack_sides(const Plan& p, const Sides& s, const Counting& c, const void* x, const void* w, float* tops, void* dx, hipStream_t st)
@@ -954,8 +986,8 @@ template <typename T>
 int run_columns(const Plan& p, const BwdArea& a, const Counted& counted, const void* x, bool with_x, const void* w, bool with_w, hipStream_t st)
 {
     const auto tiles = [&](uint32_t half) { return (int)((half / (p.f32 ? 2 : 1) + 63) / 64); };
-    const Turned<T> tw{(const T*)w, p.vocab, Counted{}, a.wt, a.wt_half, nullptr, a.tops + kTops, rows_grid(p.vocab), a.top + 1, with_w ? tiles(a.wt_half) : 0};
-    const Turned<T> tx{(const T*)x, p.rows, counted, a.xt, a.xt_half, a.dl, a.tops, rows_grid(p.rows), a.top, with_x ? tiles(a.xt_half) : 0};
+    const Turned<T> tw{(const T*)w, p.vocab, Counted{}, a.wt, a.wt_half, nullptr, a.tops + kTops, rows_grid<T>(p.vocab), a.top + 1, with_w ? tiles(a.wt_half) : 0};
+    const Turned<T> tx{(const T*)x, p.rows, counted, a.xt, a.xt_half, a.dl, a.tops, rows_grid<T>(p.rows), a.top, with_x ? tiles(a.xt_half) : 0};
     if (!(tw.tiles + tx.tiles)) return 0;
     xent_columns_kernel<T><<<dim3((unsigned)(tw.tiles + tx.tiles), (unsigned)((p.width + 63) / 64)), 256, 0, st>>>(tw, tx, p.width);
     return launched();
@@ -1023,7 +1055,7 @@ int run_product(const Job& j, int shares, hipStream_t st)
 {
     if (allow_dynamic_lds((const void*)xent_product_kernel<C, DX, OUT>, C::LDS_BYTES) != hipSuccess) return -4;
     const int tm = (int)((j.a.rows + C::BM - 1) / C::BM), tn = (int)((j.rows + C::BN - 1) / C::BN);
-    xent_product_kernel<C, DX, OUT><<<nt_grid(tm, tn) * shares, C::THREADS, C::LDS_BYTES, st>>>(j.a, j.b, j.rows, j.counted, tm, j.depth, shares,
+    xent_product_kernel<C, DX, OUT><<<(shares % 8 ? nt_grid(tm, tn) : tm * tn) * shares, C::THREADS, C::LDS_BYTES, st>>>(j.a, j.b, j.rows, j.counted, tm, j.depth, shares,
                                                                                                 (OUT*)j.out, j.ld, j.part, j.add, j.by);
     return launched();
 }

@@ -281,7 +281,7 @@ __global__ __launch_bounds__(256) void xent_columns_kernel(Turned<T> one, Turned
     const uint32_t row_half = p.row_half;
     const int64_t rows = counted.rows(p.rows), k0 = (int64_t)at * 64;
     const int c0 = blockIdx.y * 64;
-    if (k0 >= rows && counted.at) return;  // (steps that no product takes)
+    if (k0 >= rows && at) return;  // (steps that no product takes; the first one leaves the largest magnitude all the same)
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {

@@ -242,3 +242,11 @@ def test_muon_step_of_each_form(binding, shape, masters):
     # fp32: the update's share of its bound and one rounding; bf16 weights: 2^-8 and as much of the bound
     got, bound = (k, BOUND["f32"]) if masters else (w, 2.0 ** -8)
     assert (got.double().cpu() - want).norm() <= bound * want.norm()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 20, 30), (2, 65, 64), (2, 150, 333), (1, 300, 70), (40, 66, 210), (2, 200, 260), (1, 515, 260)])
+def test_what_the_workspace_holds_has_no_influence(binding, shape, dtype):
+    G, need = gradient(shape, dtype).cuda(), binding.monarch_orthogonalize_workspace_bytes(*shape, 0 if dtype == "f32" else 1)
+    a, b = (binding.monarch_orthogonalize(G, workspace=torch.full((need,), fill, dtype=torch.uint8, device="cuda")) for fill in (0, 255))
+    assert torch.isfinite(a).all() and torch.equal(a, b)

@@ -365,3 +365,19 @@ def test_a_vocabulary_that_ends_in_smaller_tiles(ops, shape, dtype):
         loss, lse = ops[1].monarch_xent_fwd(x.cuda(), W.cuda(), target.cuda(), flags=flags)
         within(loss, want.loss.cpu(), want.row_bound.cpu(), "loss")
         within(lse.cpu()[counts], want.lse.cpu()[counts], want.row_bound.cpu(), "lse")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape, ignored", [((1, 70, 33), 0.0), ((40, 300, 96), 1.0), ((150, 1100, 64), 0.3), ((150, 1100, 65), 1.0), ((300, 700, 40), 0.95)])
+def test_what_the_workspace_holds_has_no_influence(ops, shape, ignored, dtype):
+    _, binding = ops
+    x, W, target = (t.cuda() for t in inputs(*shape, dtype, ignored=ignored))
+    code, g = 0 if dtype == "f32" else 1, torch.rand((shape[0],), generator=torch.Generator().manual_seed(7)).cuda()
+    results = []
+    for fill in (0, 255):  # (255: not a number in every type)
+        ws = torch.full((binding.monarch_xent_fwd_workspace_bytes(*shape, code),), fill, dtype=torch.uint8, device="cuda")
+        loss, lse = binding.monarch_xent_fwd(x, W, target, workspace=ws)
+        ws = torch.full((binding.monarch_xent_bwd_workspace_bytes(*shape, code),), fill, dtype=torch.uint8, device="cuda")
+        results.append([loss, lse] + list(binding.monarch_xent_bwd(x, W, target, lse, g, workspace=ws)))
+    for a, b in zip(*results):
+        assert torch.isfinite(a).all() and torch.equal(a, b)

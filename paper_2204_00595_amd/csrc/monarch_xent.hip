@@ -87,15 +87,37 @@ __device__ __forceinline__ float largest_of(const float* __restrict__ v, int n)
     return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
 }
 
+// 16 bytes from wherever a row's numbers start
+__device__ __forceinline__ u32x4 loose16(const uint16_t* p)
+{
+    typedef u32x4 __attribute__((aligned(2))) loose;
+    return *reinterpret_cast<const loose*>(p);
+}
+__device__ __forceinline__ u32x4 loose16(const float* p)
+{
+    typedef u32x4 __attribute__((aligned(4))) loose;
+    return *reinterpret_cast<const loose*>(p);
+}
+
 // bf16 numbers k .. k + 7 of a row that may start anywhere; zeros from `width` on
 __device__ __forceinline__ u32x4 eight_of(const uint16_t* row, int k, int width)
 {
-    typedef u32x4 __attribute__((aligned(2))) loose;
-    if (k + 8 <= width) return *reinterpret_cast<const loose*>(row + k);
+    if (k + 8 <= width) return loose16(row + k);
     u32x4 v = {0, 0, 0, 0};
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         if (k + e < width) v[e >> 1] |= (uint32_t)row[k + e] << (16 * (e & 1));
+    return v;
+}
+
+__device__ __forceinline__ u32x4 piece_of(const uint16_t* row, int k, int width) { return eight_of(row, k, width); }
+__device__ __forceinline__ u32x4 piece_of(const float* row, int k, int width)
+{
+    if (k + 4 <= width) return loose16(row + k);
+    u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (k + e < width) v[e] = __float_as_uint(row[k + e]);
     return v;
 }
 
@@ -339,10 +361,75 @@ struct Logits {
     const int64_t* target;
     int64_t all_rows;
     Counted counted;
-    int vocab, steps, tail;
+    int vocab, width, steps, tail;
     int v0, tiles_v;           // the piece of the vocabulary: entries v0 .. of it
     __device__ __forceinline__ int64_t rows() const { return counted.rows(all_rows); }
 };
+
+// nt_product for rows of W and x that may start anywhere, as they are: 16-byte pieces by way of registers, three steps ahead, into the LDS rows that
+// nt_product has.
+template <typename C>
+__device__ __forceinline__ void loose_product(const Logits& p, int64_t rows, int64_t v0, int64_t t0, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ])
+{
+    using T = std::conditional_t<C::KIND == kF32, float, uint16_t>;
+    constexpr int PIECE = 16 / (int)sizeof(T), STEP = 8 * PIECE, AHEAD = 3, LOADS = (C::BM + C::BN) * 8 / C::THREADS, BUFFER = (C::BM + C::BN) * 128;
+    static_assert(C::PL == 1 && LOADS * C::THREADS == (C::BM + C::BN) * 8 && C::BM * 8 % C::THREADS == 0 && 2 * BUFFER <= C::LDS_BYTES, "whole passes");
+    const int tid = threadIdx.x, lane = tid & 63, piece = tid & 7, width = p.width;
+    const T* from[LOADS];  // (rows that do not exist: the last one; nobody asks for their logits)
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int r = (tid >> 3) + i * (C::THREADS / 8);
+        const int64_t v = v0 + r < p.vocab ? v0 + r : p.vocab - 1, t = t0 + r - C::BM < rows ? t0 + r - C::BM : rows - 1;
+        from[i] = i * (C::THREADS / 8) < C::BM ? (const T*)p.w.base + v * width : (const T*)p.x.base + t * width;
+    }
+#pragma unroll
+    for (int i = 0; i < C::TI; ++i)
+#pragma unroll
+        for (int j = 0; j < C::TJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    u32x4 ahead[AHEAD][LOADS];
+    const auto take = [&](int step, u32x4 (&to)[LOADS]) {
+        const int k = step * STEP + piece * PIECE;
+        if ((step + 1) * STEP <= width) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) to[i] = loose16(from[i] + k);
+        } else if (step * STEP < width) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) to[i] = piece_of(from[i], k, width);
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) take(d, ahead[d]);
+    const int r16 = lane & 15, at0 = 16 * ((lane >> 4) ^ (lane & 7)), at1 = at0 ^ 64;
+    const int fa = (C::row0() + r16) * 128, fb = (C::BM + C::col0() + r16) * 128;
+    for (int s0 = 0; s0 < p.steps; s0 += AHEAD) {
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) {
+            if (s0 + d >= p.steps) break;
+            unsigned char* buffer = lds + (s0 + d & 1) * BUFFER;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int r = (tid >> 3) + i * (C::THREADS / 8);
+                *reinterpret_cast<u32x4*>(buffer + r * 128 + 16 * (piece ^ (r & 7))) = ahead[d][i];
+            }
+            take(s0 + d + AHEAD, ahead[d]);
+            // (a barrier a step: who writes this buffer again has passed the next one, and so has everyone who reads it now)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            u32x4 b[2][C::TJ];
+#pragma unroll
+            for (int j = 0; j < C::TJ; ++j) {
+                b[0][j] = lds128(buffer + fb + j * 2048 + at0);
+                b[1][j] = lds128(buffer + fb + j * 2048 + at1);
+            }
+#pragma unroll
+            for (int i = 0; i < C::TI; ++i)
+                nt_step<C::KIND>(lds128(buffer + fa + i * 2048 + at0), lds128(buffer + fa + i * 2048 + at1), b, acc[i]);
+        }
+    }
+}
+
+enum Rows { kWhole, kTail, kLoose };  // rows of whole steps, rows that end inside one, rows that start anywhere
 
 template <typename C, bool TAIL>
 __device__ __forceinline__ void logits_tile(const Logits& p, int64_t rows, int64_t v0, int64_t t0, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ])
@@ -384,12 +471,13 @@ __device__ __forceinline__ f32x2 joined(f32x2 a, f32x2 b)
 }
 
 // Largest (in units of log 2) and sum of the tile's entries for each of its rows of x -> part[t][column]; the target's logit -> hit[t].
-template <typename C, bool TAIL>
+template <typename C, Rows ROWS>
 __device__ __forceinline__ void part_tile(const Logits& p, int64_t rows, int64_t v0, int64_t t0, unsigned char* lds, f32x2* __restrict__ part, int parts,
                                           int column, float* __restrict__ hit)
 {
     f32x4 acc[C::TI][C::TJ];
-    logits_tile<C, TAIL>(p, rows, v0, t0, lds, acc);
+    if constexpr (ROWS == kLoose) loose_product<C>(p, rows, v0, t0, lds, acc);
+    else logits_tile<C, ROWS == kTail>(p, rows, v0, t0, lds, acc);
     const int lane = threadIdx.x & 63;
     const int vr = C::row0() + 4 * (lane >> 4);
     f32x2* red = reinterpret_cast<f32x2*>(lds);  // [BM / WM][BN]
@@ -449,7 +537,7 @@ __device__ __forceinline__ void part_tile(const Logits& p, int64_t rows, int64_t
 // `columns` columns of tiles of C, and the rest of the vocabulary by tiles of S, which come last: where tiles of C fill a last round of
 // workgroups less than half, smaller ones in their place end sooner (1024 rows of width 1024, 50257 entries: 788 tiles of 256 x 256 take 116 us,
 // 768 and 80 of 128 x 128 take 104).
-template <typename C, typename S, bool TAIL>
+template <typename C, typename S, Rows ROWS>
 __global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* __restrict__ part, int parts, int columns, int groups, float* __restrict__ hit)
 {
     static_assert(S::THREADS == C::THREADS && S::LDS_BYTES <= C::LDS_BYTES, "one launch");
@@ -458,10 +546,10 @@ __global__ __launch_bounds__(C::THREADS) void xent_part_kernel(Logits p, f32x2* 
     const int64_t rows = p.rows();
     if (std::is_same_v<C, S> || (int)blockIdx.x < groups) {
         if (!nt_place(blockIdx.x, columns, (int)((rows + C::BN - 1) / C::BN), tv, tt)) return;
-        part_tile<C, TAIL>(p, rows, (int64_t)tv * C::BM, (int64_t)tt * C::BN, lds, part, parts, tv, hit);
+        part_tile<C, ROWS>(p, rows, (int64_t)tv * C::BM, (int64_t)tt * C::BN, lds, part, parts, tv, hit);
     } else {
         if (!nt_place((int)blockIdx.x - groups, parts - columns, (int)((rows + S::BN - 1) / S::BN), tv, tt)) return;
-        part_tile<S, TAIL>(p, rows, (int64_t)columns * C::BM + (int64_t)tv * S::BM, (int64_t)tt * S::BN, lds, part, parts, columns + tv, hit);
+        part_tile<S, ROWS>(p, rows, (int64_t)columns * C::BM + (int64_t)tv * S::BM, (int64_t)tt * S::BN, lds, part, parts, columns + tv, hit);
     }
 }
 
@@ -782,10 +870,13 @@ struct Plan {
     uint32_t half(int64_t k) const { return (uint32_t)((k + per_step() - 1) / per_step() * 64); }  // 16-bit numbers of an operand's row
     bool forward;  // else the gradients
     bool skips;    // ignored rows are left out
-    // Up to 64 rows the forward of fp32 tensors is bound by reading W, and the fp32 matrix instruction keeps up with that.
-    bool plain32() const { return f32 && forward && rows <= 64 && width % 4 == 0; }
-    // rows of whole 16-byte pieces serve as they are, those of x where none is left out
-    bool packs() const { return f32 ? !plain32() : width % 8 != 0; }
+    // Up to 64 rows the forward is bound by reading W, which serves as it is: the fp32 matrix instruction keeps up with that, and rows that are not
+    // whole 16-byte pieces come by way of registers (24 rows of width 767 in bf16 29 us, laid out first 54; of 1023 in fp32 53 and 218).
+    bool few() const { return forward && rows <= 64; }
+    bool plain32() const { return f32 && few(); }
+    bool loose() const { return few() && width % (f32 ? 4 : 8); }
+    // else rows of whole 16-byte pieces serve as they are, those of x where none is left out
+    bool packs() const { return !few() && (f32 || width % 8); }
     bool packs_x() const { return packs() || skips; }
     // tile of the logits: 0 = 256 x 256 (where there is one for each CU), 1 = 128 x 128, 2 = 128 entries x 64 rows, 3 = 128 x 32 (forward)
     int tile() const
@@ -1005,6 +1096,7 @@ Logits logits_of(const Plan& p, const Sides& s, const Counted& counted, const vo
     l.all_rows = p.rows;
     l.counted = counted;
     l.vocab = p.vocab;
+    l.width = p.width;
     l.steps = (int)((bytes + 127) / 128);
     l.tail = (int)(bytes % 128 / 16);
     if (!l.tail) l.tail = 8;
@@ -1016,16 +1108,19 @@ Logits logits_of(const Plan& p, const Sides& s, const Counted& counted, const vo
 template <typename C>
 int tiles_of(const Logits& l) { return (int)((l.all_rows + C::BN - 1) / C::BN); }
 // Rows that end inside a step have kernels of their own (the test for it in every step costs 14 % of a long product).
-template <typename C, bool TAIL = false>
+template <typename C, Rows ROWS = kWhole>
 int run_part(const Plan& p, const Logits& l, const FwdArea& a, hipStream_t st)
 {
-    if constexpr (!TAIL && C::KIND != kF16x2)
-        if (l.tail < 8) return run_part<C, true>(p, l, a, st);
+    if constexpr (ROWS == kWhole && C::KIND != kF16x2) {
+        if constexpr (C::BN <= 64)
+            if (p.loose()) return run_part<C, kLoose>(p, l, a, st);
+        if (l.tail < 8) return run_part<C, kTail>(p, l, a, st);
+    }
     using S = std::conditional_t<C::BM == 256, std::conditional_t<C::KIND == kBf16, End, End2>, C>;
-    if (allow_dynamic_lds((const void*)xent_part_kernel<C, S, TAIL>, C::LDS_BYTES) != hipSuccess) return -4;
+    if (allow_dynamic_lds((const void*)xent_part_kernel<C, S, ROWS>, C::LDS_BYTES) != hipSuccess) return -4;
     const int columns = p.columns(), parts = p.forward_parts(), groups = nt_grid(columns, tiles_of<C>(l));
     const int end = parts > columns ? nt_grid(parts - columns, tiles_of<S>(l)) : 0;
-    xent_part_kernel<C, S, TAIL><<<groups + end, C::THREADS, C::LDS_BYTES, st>>>(l, a.part, parts, columns, groups, a.hit);
+    xent_part_kernel<C, S, ROWS><<<groups + end, C::THREADS, C::LDS_BYTES, st>>>(l, a.part, parts, columns, groups, a.hit);
     return launched();
 }
 template <typename C, bool TAIL = false, bool PAST = false>

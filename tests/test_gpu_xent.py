@@ -381,3 +381,14 @@ def test_what_the_workspace_holds_has_no_influence(ops, shape, ignored, dtype):
         results.append([loss, lse] + list(binding.monarch_xent_bwd(x, W, target, lse, g, workspace=ws)))
     for a, b in zip(*results):
         assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 200, 1), (2, 300, 31), (20, 260, 702), (32, 129, 197), (33, 129, 5), (50, 300, 77), (63, 1000, 385), (64, 127, 130)])
+def test_few_rows_that_start_anywhere(ops, shape, dtype):
+    """Forward of up to 64 rows whose width is no whole number of 16-byte pieces: one step and less, several, each of the two tiles."""
+    x, W, target = inputs(*shape, dtype, ignored=0.2 if shape[0] > 2 else 0.0)
+    want, counts = Exact(x, W, target, torch.ones(shape[0]), dtype), target != IGNORE
+    loss, lse = ops[1].monarch_xent_fwd(x.cuda(), W.cuda(), target.cuda())
+    within(loss, want.loss, want.row_bound, "loss")
+    within(lse.cpu()[counts], want.lse[counts], want.row_bound, "lse")

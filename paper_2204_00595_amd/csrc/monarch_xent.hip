@@ -878,21 +878,32 @@ struct Plan {
     // else rows of whole 16-byte pieces serve as they are, those of x where none is left out
     bool packs() const { return !few() && (f32 || width % 8); }
     bool packs_x() const { return packs() || skips; }
-    // tile of the logits: 0 = 256 x 256 (where there is one for each CU), 1 = 128 x 128, 2 = 128 entries x 64 rows, 3 = 128 x 32 (forward)
+    // tile of the logits: 0 = 256 x 256, 1 = 128 x 128 (whichever is estimated to end sooner, as in cut_for: 600 rows of width 768, 50257 entries
+    // 62 us by 128, 74 by 256; 1024 of width 1024 121 and 103), 2 = 128 entries x 64 rows, 3 = 128 x 32 (forward)
     int tile() const
     {
-        if (rows > 128 && ((rows + 255) / 256) * ((vocab + 255) / 256) >= 256) return 0;
-        return rows > 64 ? 1 : rows > 32 || !forward ? 2 : 3;
+        if (rows <= 128) return rows > 64 ? 1 : rows > 32 || !forward ? 2 : 3;
+        const int64_t big = ((rows + 255) / 256) * ((vocab + 255) / 256), mid = ((rows + 127) / 128) * ((vocab + 127) / 128);
+        const double steps = (width + per_step() - 1) / per_step();
+        const double alone = 0.55 * steps + 3, by_mid = mid <= 256 ? alone : (mid + 511) / 512 * (0.9 * steps + 3);
+        const double by_big = ends() ? big / 256 * (1.6 * steps + 4) + alone : (big + 255) / 256 * (1.6 * steps + 4);
+        return by_big <= by_mid ? 0 : 1;
+    }
+    // Columns of 256 x 256 tiles in whole rounds; what is left of the forward's ends sooner by tiles of 128 if those are at most one round.
+    int whole_columns() const
+    {
+        const int64_t across = (rows + 255) / 256;
+        return (int)((vocab + 255) / 256 * across / 256 * 256 / across);
+    }
+    bool ends() const
+    {
+        const int64_t rest = (vocab + 255) / 256 - whole_columns();
+        return forward && whole_columns() > 0 && rest > 0 && rest * ((rows + 255) / 256) * 4 <= 256;
     }
     int bv() const { return tile() == 0 ? 256 : 128; }
     int bt() const { return tile() == 0 ? 256 : tile() == 1 ? 128 : tile() == 2 ? 64 : 32; }
     int parts() const { return (vocab + bv() - 1) / bv(); }
-    // The forward's tiles of 256 x 256 end with a round that is at most half full: columns before that round, else all.
-    int columns() const
-    {
-        const int64_t all = parts(), across = row_tiles(), whole = all * across / 256 * 256 / across;
-        return tile() == 0 && whole > 0 && (all - whole) * across * 4 <= 256 ? (int)whole : (int)all;
-    }
+    int columns() const { return tile() == 0 && ends() ? whole_columns() : parts(); }
     int forward_parts() const { return columns() == parts() ? parts() : columns() + (vocab - columns() * bv() + 127) / 128; }
     int64_t row_tiles() const { return (rows + bt() - 1) / bt(); }
 };

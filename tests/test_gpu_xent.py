@@ -392,3 +392,9 @@ def test_few_rows_that_start_anywhere(ops, shape, dtype):
     loss, lse = ops[1].monarch_xent_fwd(x.cuda(), W.cuda(), target.cuda())
     within(loss, want.loss, want.row_bound, "loss")
     within(lse.cpu()[counts], want.lse[counts], want.row_bound, "lse")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(512, 33500, 40), (1000, 17000, 33)])
+def test_the_same_with_rows_that_fill_the_tiles(ops, shape, dtype):
+    test_a_vocabulary_that_ends_in_smaller_tiles(ops, shape, dtype)

@@ -841,7 +841,6 @@ using End2 = NtTile<128, 128, 64, 32, kF16x2>;
 using Big2 = NtTile<256, 256, 128, 64, kF16x2>;
 using Mid2 = NtTile<128, 128, 64, 64, kF16x2>;
 using Low2 = NtTile<128, 64, 32, 64, kF16x2>;
-using Few2 = NtTile<128, 32, 32, 32, kF16x2>;
 using Low32 = NtTile<128, 64, 32, 64, kF32, 3>;
 using Few32 = NtTile<128, 32, 32, 32, kF32, 4>;
 using Big16 = NtTile<256, 256, 128, 64, kF16>;
@@ -1216,7 +1215,7 @@ int xent_fwd(const void* x, const void* w, const int64_t* target, float* loss, f
     if (rc) return rc;
     const Logits l = logits_of(p, a.sides, counted, x, w, target);
     if (p.plain32()) rc = p.rows > 32 ? run_part<Low32>(p, l, a, st) : run_part<Few32>(p, l, a, st);
-    else if (p.f32) rc = by_tile<Big2, Mid2, Low2, Few2>(p, [&](auto c) { return run_part<decltype(c)>(p, l, a, st); });
+    else if (p.f32) rc = p.tile() ? run_part<Mid2>(p, l, a, st) : run_part<Big2>(p, l, a, st);
     else rc = by_tile<Big, Mid, Low, FewB>(p, [&](auto c) { return run_part<decltype(c)>(p, l, a, st); });
     if (rc) return rc;
     xent_join_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a.part, p.forward_parts(), a.hit, target, ignore, vocab, rows, counted, loss, lse);

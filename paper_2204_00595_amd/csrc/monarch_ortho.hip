@@ -683,15 +683,17 @@ int product(const Product& p, const Sink& sink, hipStream_t st)
 }
 
 // Two launches a step instead of three where a launch costs most: up to 512 slabs (two workgroups of four waves for each CU), or blocks near squares, whose
-// P costs as much as the second product with A.  Five steps, two launches a step against three: 16 blocks of 192 x 192 81 against 88 us, 64 of
-// 128 x 128 77 / 89, 128 of 128 x 128 103 / 120, 16 of 192 x 512 (512 slabs) 111 / 120; past the rule, 24 of 192 x 384 (576 slabs) 127 / 115 and
-// 64 of 192 x 768 377 / 254.
-bool by_slabs(const OrthoArea& a, int64_t blocks) { return a.r <= 192 && ((a.c + 15) / 16 * blocks <= 512 || 4 * a.c <= 5 * a.r); }
+// P costs as much as the second product with A, and any blocks of up to 64.  Five steps, two launches a step against three: 16 blocks of
+// 192 x 192 81 against 88 us, 64 of 128 x 128 77 / 89, 128 of 128 x 128 103 / 120, 16 of 192 x 512 (512 slabs) 111 / 120, 40 of 64 x 600
+// 76 / 98, 200 of 64 x 800 210 / 208; past the rule, 24 of 192 x 384 (576 slabs) 127 / 115, 64 of 100 x 600 170 / 147 and 64 of 192 x 768
+// 377 / 254.
+bool by_slabs(const OrthoArea& a, int64_t blocks) { return a.r <= 64 || (a.r <= 192 && ((a.c + 15) / 16 * blocks <= 512 || 4 * a.c <= 5 * a.r)); }
 template <bool LAST, bool TALL, typename T, Out OUT>
 int run_apply(const Apply& p, const Sink& sink, hipStream_t st)
 {
     const unsigned grid = (unsigned)((p.slabs * p.blocks + 7) / 8 * 8);
-    if (p.r <= 128) ortho_apply_kernel<128, LAST, TALL, T, OUT><<<grid, 256, 0, st>>>(p, sink);
+    if (p.r <= 64) ortho_apply_kernel<64, LAST, TALL, T, OUT><<<grid, 256, 0, st>>>(p, sink);
+    else if (p.r <= 128) ortho_apply_kernel<128, LAST, TALL, T, OUT><<<grid, 256, 0, st>>>(p, sink);
     else ortho_apply_kernel<192, LAST, TALL, T, OUT><<<grid, 256, 0, st>>>(p, sink);
     return launched();
 }

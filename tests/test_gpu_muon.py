@@ -250,3 +250,12 @@ def test_what_the_workspace_holds_has_no_influence(binding, shape, dtype):
     G, need = gradient(shape, dtype).cuda(), binding.monarch_orthogonalize_workspace_bytes(*shape, 0 if dtype == "f32" else 1)
     a, b = (binding.monarch_orthogonalize(G, workspace=torch.full((need,), fill, dtype=torch.uint8, device="cuda")) for fill in (0, 255))
     assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(39, 16, 592), (30, 333, 64), (26, 126, 11), (12, 33, 1000), (40, 100, 600)])
+def test_many_slabs(binding, shape, dtype):
+    G = gradient(shape, dtype)
+    X = binding.monarch_orthogonalize(G.cuda())
+    assert far(X, orthogonal(G)) <= BOUND[dtype]
+    assert torch.equal(X, binding.monarch_orthogonalize(G.cuda()))

@@ -202,8 +202,8 @@ struct Counting {  // the rows of x that count; what is kept of them
 };
 
 // The rows of x and of W (groups of workgroups beside one another).  Each workgroup of x takes rows that follow one another and counts by
-// itself which of those before them count, so that no launch comes before this one (as launches of their own, three for a forward and three
-// for a backward of 777 rows of width 330, 8191 entries: 10 us more).  `zero` (may be null): the rows of dx that do not count become zero.
+// itself which of those before them count, so that no launch comes before this one (as launches of their own, with those of the columns: a
+// training step on 777 rows of width 330, 8191 entries, 110 us for 87).  `zero` (may be null): the rows of dx that do not count become zero.
 template <typename T>
 __global__ __launch_bounds__(64 * kRowWaves<T>) void xent_rows_kernel(Taken<T> x, Counting c, Taken<T> w, int width, uint32_t row_half, T* __restrict__ zero)
 {
